@@ -58,7 +58,8 @@ enum {
     EA_ERR_DTYPE = -4,      /* unknown ea_dtype */
     EA_ERR_WORKSPACE = -5,  /* workspace NULL, misaligned or too small */
     EA_ERR_HIP = -6,        /* a HIP call failed; see entmax_attn_last_hip_error() */
-    EA_ERR_TOO_LARGE = -7   /* the problem needs more scratch than an allocation-free entry point holds */
+    EA_ERR_TOO_LARGE = -7,  /* the problem needs more scratch than an allocation-free entry point holds */
+    EA_ERR_LAYOUT = -8      /* a pointer or stride is not a multiple of 16 bytes, a stride is negative, or rows that are written overlap */
 };
 
 /* The workspace starts with EA_STATS_COPIES copies of EA_STATS_WORDS 64-bit counters
@@ -227,6 +228,120 @@ size_t entmax_attn_decode_static_max_bytes(void);
 int entmax_attn_decode_static(const void* q, const void* K, const void* V,
                               float* O, float* tau, int32_t* support, int32_t* iters,
                               int B, int H, int N, int d, int dtype, float alpha, void* hip_stream);
+
+/*
+ * Queries and keys as entmax_attn_fwd takes them, from what a layer's projections give: the RMS norm
+ * of each head's row and its rotation by the token's position, in one pass.
+ *     y = w x / sqrt(mean(x^2) + eps)                               (norm != 0; else y = x)
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = position[axis(i)] * inv_freq[i]
+ * for the pairs i = 0 .. rot/2 - 1 of the row's first `rot` elements: (i, i + rot/2), or the neighbours
+ * (2i, 2i + 1) if `interleaved`; elements from `rot` on are not rotated.  Pairs are dealt to n_axes position
+ * axes in order: the first sections[0] pairs turn with the first axis, the next sections[1] with the
+ * second, and so on (text: one axis; images and video: height and width, or time, height and width).
+ *   q, k        in   [B,N,Hq,d], [B,N,Hk,d] of `dtype`, elements of a row contiguous; q_strides, k_strides: HOST
+ *                    pointers to three strides each (batch, token, head), in elements, not negative; 0
+ *                    repeats a row.  Views of one projection's rows are what they are for.
+ *   q_out, k_out out [B,Hq,N,d], [B,Hk,N,d] of `dtype`, contiguous (N = 1: what entmax_attn_decode takes as q)
+ *   q_weight, k_weight in [d] float32, may be NULL (ones); they go with norm != 0
+ *   positions   in   [n_axes,B,N] int32, any value;  inv_freq in [rot/2] float32 (both unused if rot = 0)
+ *   sections    in   HOST pointer to n_axes pair counts that sum to rot/2; may be NULL for one axis
+ * Angles are formed in 64 bits from the int32 position and the float32 frequency; everything else is in float32,
+ * rounded once to `dtype`.  B N <= 2^27, d 64 or 128, rot a multiple of 8 (0 .. d), at most 4 axes, eps > 0.
+ * EA_ERR_LAYOUT if q, k, an output, a weight or a stride is not a multiple of 16 bytes.
+ *
+ * entmax_attn_qk_norm_rope_bwd: the gradient.  It takes dQ, dK as entmax_attn_bwd returns them.
+ *   dq_out, dk_out in [B,Hq,N,d], [B,Hk,N,d] float32, contiguous
+ *   dq, dk      out  like q, k, of `dtype`, with strides of their own (rows must not overlap); for an input whose rows
+ *                    repeat (stride 0) they hold the gradient of each use
+ *   dq_weight, dk_weight out [d] float32, overwritten; NULL where not wanted
+ *   workspace        entmax_attn_qk_norm_rope_workspace_bytes(d) bytes, 256-byte aligned; may be NULL if no
+ *                    weight gradient is wanted
+ * Results repeat bit for bit.  No output may overlap an input.
+ */
+int entmax_attn_qk_norm_rope_fwd(const void* q, const void* k, void* q_out, void* k_out,
+                                 const int64_t* q_strides, const int64_t* k_strides,
+                                 const float* q_weight, const float* k_weight, const int32_t* positions, const float* inv_freq,
+                                 int B, int Hq, int Hk, int N, int d, int dtype,
+                                 int rot, int n_axes, const int* sections, int interleaved, int norm, float eps, void* hip_stream);
+size_t entmax_attn_qk_norm_rope_workspace_bytes(int d);
+int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_out, const float* dk_out, void* dq, void* dk,
+                                 const int64_t* q_strides, const int64_t* k_strides, const int64_t* dq_strides, const int64_t* dk_strides,
+                                 const float* q_weight, const float* k_weight, const int32_t* positions, const float* inv_freq,
+                                 float* dq_weight, float* dk_weight,
+                                 int B, int Hq, int Hk, int N, int d, int dtype,
+                                 int rot, int n_axes, const int* sections, int interleaved, int norm, float eps,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A paged key/value cache in 4 bits, for serving: requests of different lengths, each a list of pages.
+ *
+ * Format.  `cache` is [n_pages][entmax_attn_cache4_page_bytes(Hk, d, page_size)] bytes, 16-byte aligned.  A page holds
+ * page_size (16, 32, 64, 128 or 256) tokens of all Hk key/value heads; head h's part starts at h times
+ * page_size * 17 d / 16 bytes and is
+ *     key codes [page_size][d/2], key scales [page_size][d/32], value codes [page_size][d/2], value scales [page_size][d/32].
+ * 32 neighbouring values share the scale 2^(byte - 127); a code is a sign bit above three bits that stand for
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6; the value with the lower index is in the lower half of its byte.  A slot is
+ * page * page_size + (token within the page); n_pages * page_size < 2^31.
+ *
+ * entmax_attn_cache_tables: one step of a scheduler, on the GPU.  Request r goes from lens[r] cached tokens to
+ * new_lens[r]: more (a prompt, a chunk of one, a token), fewer (an ended request: 0; a draft that was not accepted),
+ * or as many.
+ *   lens, new_lens in  [R] int32
+ *   block_table in/out [R][max_blocks] int32: the pages of each request in the order of its tokens; entries behind them are
+ *                      left as they were
+ *   free_pages, free_count in/out [n_pages], [1] int32: a stack of the free pages.  First the pages that shrinking requests
+ *                      leave go on top, the last request's last page first; then the growing requests, in order, take
+ *                      theirs from the top.  (A step and the step back leave the stack as it was.)
+ *   lens_out    out    [R] int32: the length the request has now; may be `lens` itself, not new_lens
+ *   token_start out    [R+1] int32: the new tokens of request r are the rows token_start[r] .. token_start[r+1] - 1 of a batch
+ *                      of new tokens, whether they were granted or not
+ *   slots, positions out [max_tokens] int32: each row's slot and position in its request; slot -1 in the rows of a
+ *                      request that was refused, and slot -1, position 0 in the rows behind the last
+ *   status      out    [4] int32: rows in use (at most max_tokens), requests refused, requests with a length that is negative or
+ *                      above max_blocks * page_size (nothing is done for them), page ids outside 0 .. n_pages - 1 met
+ * A request that wants more pages than are left after the requests before it, or whose rows end behind max_tokens, is
+ * refused whole: its length and pages stay, and so it is for the later ones that want any (pages; rows).  R <= 4096,
+ * max_blocks * page_size <= 2^22.  The pages of a request must be its own: the call cannot tell.
+ *
+ * entmax_attn_cache4_write: keys and values of T tokens to their slots.
+ *   K, V        in   rows [T][Hk][d] of `dtype`; k_strides, v_strides: HOST pointers to two strides each (token, head), in elements
+ *   slots       in   [T] int32; a row whose slot is negative or past the cache is skipped.  The slots of a call must
+ *                    differ: of two rows with one slot, either's codes and scales may stand there.
+ * A block's scale is 2^s, s = floor(log2 max|x|) - 2, or one more where max|x| > 7 * 2^s, within 2^-126 .. 2^125; x / 2^s
+ * is rounded to the nearest code, ties to the even one, above 6 to 6.  A block that holds an infinity or a NaN gets
+ * scale byte 255 and reads as NaN.
+ *
+ * entmax_attn_cache4_read: the rows of T slots as the cache holds them (exact in either type), for attention over cached keys with
+ * entmax_attn_fwd, or to move requests.  Rows of K, V whose slot is negative or past the cache are left as they were.
+ * T = 0 is allowed in both and does nothing.
+ *
+ * entmax_attn_decode_cache4: entmax_attn_decode against the cache: one query per head and request.
+ *   q           in   [R,Hq,d] of `dtype`; Hq is a multiple of Hk, query head h attends to head h / (Hq / Hk)
+ *   block_table in   [R][max_blocks], lens in [R] int32: request r has the first lens[r] tokens of its pages.
+ *   O           out  [R,Hq,d] float32;  tau out [R,Hq] float32, raw convention as in entmax_attn_fwd
+ *   support     out  [R,Hq] int32, may be NULL: number of keys with p > 0
+ *   max_len          at least the largest length, at most 2^22 and max_blocks * page_size: the launch and the workspace go by it
+ * A request of length 0 gets O = 0, tau = 0, support 0.  One whose length is negative or above max_len, or that has a
+ * page id outside 0 .. n_pages - 1 among the pages it attends to, gets NaN and support -1, and so does a head with a score
+ * that is infinite or NaN.  What the cache holds behind a request's last token has no effect.
+ * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or four (float32) 8-bit terms: a bf16
+ * element is exact down to 2^-13 of the largest of its row and known to 2^-21 of that below, a float32 element
+ * to 2^-26 of it (rows whose largest element is below 2^-100 lose more); the rest is in float32.
+ * Results repeat bit for bit.  Two calls at once need two workspaces.
+ */
+size_t entmax_attn_cache4_page_bytes(int Hk, int d, int page_size);      /* 0 for a bad shape */
+int entmax_attn_cache_tables(const int32_t* lens, const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
+                             int32_t* free_count, int32_t* lens_out, int32_t* token_start, int32_t* slots, int32_t* positions,
+                             int32_t* status, int R, int max_blocks, int page_size, int n_pages, int max_tokens, void* hip_stream);
+int entmax_attn_cache4_write(const void* K, const void* V, const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                             void* cache, int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream);
+int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
+                            int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream);
+size_t entmax_attn_decode_cache4_workspace_bytes(int R, int Hq, int Hk, int d, int max_len);     /* 0 for a bad shape */
+int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* block_table, const int32_t* lens,
+                              float* O, float* tau, int32_t* support,
+                              int R, int Hq, int Hk, int d, int dtype, int max_len, int max_blocks, int n_pages, int page_size,
+                              float alpha, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Static, human-readable text for a return code. */
 const char* entmax_attn_strerror(int code);

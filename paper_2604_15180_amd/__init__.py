@@ -8,4 +8,7 @@ from .binding import (  # noqa: F401
     entmax_attn_decode, entmax_attn_decode_workspace_bytes, entmax_attn_gather_enable,
     entmax_attn_decode_static, entmax_attn_decode_static_max_bytes, entmax_attn_fwd_histogram_bounds,
     entmax_attn_right_edge_enable, entmax_attn_coissue_probe,
+    entmax_attn_qk_norm_rope_fwd, entmax_attn_qk_norm_rope_bwd, entmax_attn_qk_norm_rope_workspace_bytes,
+    entmax_attn_cache_tables, entmax_attn_cache4_empty, entmax_attn_cache4_page_bytes, entmax_attn_cache4_write,
+    entmax_attn_cache4_read, entmax_attn_decode_cache4, entmax_attn_decode_cache4_workspace_bytes,
 )

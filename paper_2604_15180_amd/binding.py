@@ -83,6 +83,24 @@ def lib():
         L.entmax_attn_mfma_probe.argtypes = [vp, vp, ci, ci, vp]
         L.entmax_attn_coissue_probe.restype = ci
         L.entmax_attn_coissue_probe.argtypes = [vp, ci, ci, ci, vp]
+        L.entmax_attn_qk_norm_rope_fwd.restype = ci
+        L.entmax_attn_qk_norm_rope_fwd.argtypes = [vp] * 10 + [ci] * 8 + [vp, ci, ci, cf, vp]
+        L.entmax_attn_qk_norm_rope_workspace_bytes.restype = sz
+        L.entmax_attn_qk_norm_rope_workspace_bytes.argtypes = [ci]
+        L.entmax_attn_qk_norm_rope_bwd.restype = ci
+        L.entmax_attn_qk_norm_rope_bwd.argtypes = [vp] * 16 + [ci] * 8 + [vp, ci, ci, cf, vp, sz, vp]
+        L.entmax_attn_cache4_page_bytes.restype = sz
+        L.entmax_attn_cache4_page_bytes.argtypes = [ci, ci, ci]
+        L.entmax_attn_cache_tables.restype = ci
+        L.entmax_attn_cache_tables.argtypes = [vp] * 10 + [ci] * 5 + [vp]
+        L.entmax_attn_cache4_write.restype = ci
+        L.entmax_attn_cache4_write.argtypes = [vp] * 6 + [ci] * 6 + [vp]
+        L.entmax_attn_cache4_read.restype = ci
+        L.entmax_attn_cache4_read.argtypes = [vp] * 6 + [ci] * 6 + [vp]
+        L.entmax_attn_decode_cache4_workspace_bytes.restype = sz
+        L.entmax_attn_decode_cache4_workspace_bytes.argtypes = [ci] * 5
+        L.entmax_attn_decode_cache4.restype = ci
+        L.entmax_attn_decode_cache4.argtypes = [vp] * 7 + [ci] * 9 + [cf, vp, sz, vp]
         L.entmax_attn_strerror.restype = ctypes.c_char_p
         L.entmax_attn_strerror.argtypes = [ci]
         _lib = L
@@ -269,6 +287,245 @@ def entmax_attn_decode(q, K, V, alpha, workspace=None):
                                     B, H, N, d, _dtype_code(K.dtype), float(alpha), _ptr(ws), ws.numel(),
                                     ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)))
     return O, tau, support, iters
+
+
+# ---- queries and keys from a layer's projections; the 4-bit cache --------------------------------
+
+def _on_gpu(call, *tensors):
+    """The one device of the tensors (None is skipped), made current for the launch by the caller's `with`."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{call}: tensors must live on the GPU (there is no CPU path)")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{call}: tensors on {dev} and {t.device}")
+    return dev
+
+
+class _Launch:
+    """Launches go to the current stream of the tensors' device, with that device current."""
+    __slots__ = ("dev", "before")
+
+    def __init__(self, dev):
+        self.dev = dev.index
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.dev:
+            torch.cuda.set_device(self.dev)
+        return torch.cuda.current_stream(self.dev).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.dev:
+            torch.cuda.set_device(self.before)
+
+
+def _int32(call, name, t, shape):
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{call}: {name} must be contiguous int32 {list(shape)}, got {t.dtype} {list(t.shape)}")
+
+
+def _strides(*n):
+    return (ctypes.c_int64 * len(n))(*n)
+
+
+def _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections):
+    if q.dim() != 4 or k.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3] or q.dtype != k.dtype:
+        raise ValueError(f"{call}: q [B,N,Hq,d], k [B,N,Hk,d] of one dtype")
+    if q.stride(3) != 1 or k.stride(3) != 1:
+        raise ValueError(f"{call}: the elements of a row of q and k must be contiguous")
+    B, N, Hq, d = q.shape
+    rot = axes = 0
+    if inv_freq is not None and inv_freq.numel() > 0:
+        rot = 2 * inv_freq.numel()
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise ValueError(f"{call}: inv_freq must be contiguous float32 [rot / 2]")
+        if positions is None:
+            raise ValueError(f"{call}: inv_freq without positions")
+        axes = positions.shape[0] if positions.dim() == 3 else 1
+        _int32(call, "positions", positions, (axes, B, N) if positions.dim() == 3 else (B, N))
+        if sections is not None and len(sections) != axes:
+            raise ValueError(f"{call}: {len(sections)} sections for {axes} position axes")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
+            raise ValueError(f"{call}: a weight must be contiguous float32 [{d}]")
+    if not norm and (q_weight is not None or k_weight is not None):
+        raise ValueError(f"{call}: weights go with norm=True")
+    sec = (ctypes.c_int * axes)(*sections) if rot and sections is not None else None
+    return B, N, Hq, k.shape[2], d, rot, axes, sec
+
+
+def _row_strides(t):
+    return _strides(t.stride(0), t.stride(1), t.stride(2))
+
+
+def entmax_attn_qk_norm_rope_fwd(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, norm=True, sections=None,
+                                 interleaved=False):
+    """q [B,N,Hq,d], k [B,N,Hk,d] (any strides between rows) -> q_out [B,Hq,N,d], k_out [B,Hk,N,d], normed per head
+    and rotated.  positions: int32 [B,N], or [axes,B,N] with `sections` pairs for each axis; inv_freq: float32 [rot / 2], None
+    for no rotation."""
+    call = "entmax_attn_qk_norm_rope_fwd"
+    dev = _on_gpu(call, q, k, positions, inv_freq, q_weight, k_weight)
+    B, N, Hq, Hk, d, rot, axes, sec = _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections)
+    q_out = torch.empty((B, Hq, N, d), dtype=q.dtype, device=dev)
+    k_out = torch.empty((B, Hk, N, d), dtype=q.dtype, device=dev)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_qk_norm_rope_fwd(
+            _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _row_strides(q), _row_strides(k), _ptr(q_weight), _ptr(k_weight),
+            _ptr(positions), _ptr(inv_freq), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, int(bool(interleaved)),
+            int(bool(norm)), float(eps), stream))
+    return q_out, k_out
+
+
+def entmax_attn_qk_norm_rope_workspace_bytes(d):
+    return int(lib().entmax_attn_qk_norm_rope_workspace_bytes(d))
+
+
+def entmax_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, norm=True,
+                                 sections=None, interleaved=False, out=None, workspace=None):
+    """The gradient: dq_out [B,Hq,N,d], dk_out [B,Hk,N,d] float32 (entmax_attn_bwd's dQ, dK) -> (dq, dk, dq_weight, dk_weight),
+    dq, dk like q, k (contiguous, or `out` = (dq, dk) views to write into), weight gradients float32 [d], None for a weight that
+    was None."""
+    call = "entmax_attn_qk_norm_rope_bwd"
+    dev = _on_gpu(call, q, k, dq_out, dk_out, positions, inv_freq, q_weight, k_weight, workspace, *(out or ()))
+    B, N, Hq, Hk, d, rot, axes, sec = _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections)
+    for g, H in ((dq_out, Hq), (dk_out, Hk)):
+        if g.dtype != torch.float32 or tuple(g.shape) != (B, H, N, d) or not g.is_contiguous():
+            raise ValueError(f"{call}: dq_out, dk_out must be contiguous float32 [B,H,N,d]")
+    if out is None:
+        dq, dk = (torch.empty((B, N, H, d), dtype=q.dtype, device=dev) for H in (Hq, Hk))
+    else:
+        dq, dk = out
+        if dq.shape != q.shape or dk.shape != k.shape or dq.dtype != q.dtype or dk.dtype != q.dtype or dq.stride(3) != 1 or dk.stride(3) != 1:
+            raise ValueError(f"{call}: out must be of q's and k's shapes and dtype, rows contiguous")
+    dwq, dwk = (None if w is None else torch.empty(d, dtype=torch.float32, device=dev) for w in (q_weight, k_weight))
+    ws = workspace
+    if ws is None and (dwq is not None or dwk is not None):
+        ws = _workspace(entmax_attn_qk_norm_rope_workspace_bytes(d), dev)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_qk_norm_rope_bwd(
+            _ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _row_strides(q), _row_strides(k), _row_strides(dq),
+            _row_strides(dk), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(inv_freq), _ptr(dwq), _ptr(dwk),
+            B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, int(bool(interleaved)), int(bool(norm)), float(eps),
+            _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), stream))
+    return dq, dk, dwq, dwk
+
+
+def entmax_attn_cache_tables(lens, new_lens, block_table, free_pages, free_count, page_size, max_tokens, out=None):
+    """One scheduler step on the GPU: requests go from lens [R] to new_lens [R] tokens.  block_table [R,max_blocks], the stack
+    free_pages [n_pages] and free_count [1] (all int32) are updated in place -> (lens_out [R], token_start [R+1], slots
+    [max_tokens], positions [max_tokens], status [4]), int32; `out`: tensors to write them into (lens_out may be lens)."""
+    call = "entmax_attn_cache_tables"
+    dev = _on_gpu(call, lens, new_lens, block_table, free_pages, free_count, *(out or ()))
+    if block_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError(f"{call}: block_table [R,max_blocks], free_pages [n_pages]")
+    R, blocks = block_table.shape
+    shapes = ((R,), (R + 1,), (max_tokens,), (max_tokens,), (4,))
+    for name, t, shape in (("lens", lens, (R,)), ("new_lens", new_lens, (R,)), ("block_table", block_table, (R, blocks)),
+                           ("free_pages", free_pages, free_pages.shape), ("free_count", free_count, (1,))):
+        _int32(call, name, t, shape)
+    if out is None:
+        both = torch.empty(2 * R + 5 + 2 * max(max_tokens, 0), dtype=torch.int32, device=dev)
+        out = both.split([R, R + 1, max_tokens, max_tokens, 4]) if max_tokens >= 0 else (both,) * 5
+    else:
+        for name, t, shape in zip(("lens_out", "token_start", "slots", "positions", "status"), out, shapes):
+            _int32(call, name, t, shape)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_cache_tables(
+            _ptr(lens), _ptr(new_lens), _ptr(block_table), _ptr(free_pages), _ptr(free_count), *(_ptr(t) for t in out),
+            R, blocks, page_size, free_pages.numel(), max_tokens, stream))
+    return tuple(out)
+
+
+def entmax_attn_cache4_page_bytes(Hk, d, page_size):
+    return int(lib().entmax_attn_cache4_page_bytes(Hk, d, page_size))
+
+
+def entmax_attn_cache4_empty(n_pages, Hk, d, page_size, device="cuda"):
+    """A cache of n_pages pages: uint8 [n_pages, Hk, page_size * 17 d / 16], all values zero."""
+    nbytes = entmax_attn_cache4_page_bytes(Hk, d, page_size)
+    if nbytes == 0 or n_pages <= 0:
+        raise ValueError("entmax_attn_cache4_empty: Hk, n_pages > 0, d 64 or 128, page_size 16, 32, 64, 128 or 256")
+    return torch.zeros((n_pages, Hk, nbytes // Hk), dtype=torch.uint8, device=device)
+
+
+def _cache_args(call, cache, d, page_size):
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.shape[2] * 16 != page_size * d * 17:
+        raise ValueError(f"{call}: cache must be contiguous uint8 [n_pages, Hk, page_size * 17 d / 16]")
+    return cache.shape[0], cache.shape[1]
+
+
+def _cache_rows(call, k, v, slots, Hk):
+    if k.dim() != 3 or k.shape != v.shape or k.shape[1] != Hk or k.dtype != v.dtype:
+        raise ValueError(f"{call}: K, V must be [T,Hk,d] of one dtype, with the cache's Hk")
+    if k.numel() and (k.stride(2) != 1 or v.stride(2) != 1):
+        raise ValueError(f"{call}: the elements of a row must be contiguous")
+    _int32(call, "slots", slots, (k.shape[0],))
+    return _strides(k.stride(0), k.stride(1)), _strides(v.stride(0), v.stride(1))
+
+
+def entmax_attn_cache4_write(K, V, slots, cache, page_size):
+    """K, V [T,Hk,d] (any strides between rows) to the slots [T] (int32; negative: skipped) of a 4-bit cache."""
+    call = "entmax_attn_cache4_write"
+    dev = _on_gpu(call, K, V, slots, cache)
+    d = K.shape[-1]
+    pages, Hk = _cache_args(call, cache, d, page_size)
+    ks, vs = _cache_rows(call, K, V, slots, Hk)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_cache4_write(_ptr(K), _ptr(V), ks, vs, _ptr(slots), _ptr(cache), K.shape[0], Hk, d,
+                                              _dtype_code(K.dtype), pages, page_size, stream))
+
+
+def entmax_attn_cache4_read(cache, slots, page_size, d, dtype=torch.bfloat16, out=None):
+    """The rows of the slots [T] as the cache holds them -> (K, V) [T,Hk,d]; `out` = (K, V) to write into (any strides between
+    rows; rows of negative slots are left as they were, and are undefined without `out`)."""
+    call = "entmax_attn_cache4_read"
+    dev = _on_gpu(call, cache, slots, *(out or ()))
+    pages, Hk = _cache_args(call, cache, d, page_size)
+    if out is None:
+        out = tuple(torch.empty((slots.numel(), Hk, d), dtype=dtype, device=dev) for _ in range(2))
+    K, V = out
+    if K.shape[-1] != d:
+        raise ValueError(f"{call}: out must be [T,Hk,{d}]")
+    ks, vs = _cache_rows(call, K, V, slots, Hk)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_cache4_read(_ptr(cache), _ptr(slots), _ptr(K), _ptr(V), ks, vs, K.shape[0], Hk, d,
+                                             _dtype_code(K.dtype), pages, page_size, stream))
+    return K, V
+
+
+def entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len):
+    return int(lib().entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len))
+
+
+def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max_len=None, workspace=None):
+    """One query per head and request against a 4-bit cache: q [R,Hq,d], block_table [R,max_blocks], lens [R] (int32) ->
+    (O [R,Hq,d], tau [R,Hq], support [R,Hq]).  max_len: the largest length there can be (default: all that the table's pages
+    hold); launch and workspace go by it."""
+    call = "entmax_attn_decode_cache4"
+    dev = _on_gpu(call, q, cache, block_table, lens, workspace)
+    if q.dim() != 3 or not q.is_contiguous() or block_table.dim() != 2:
+        raise ValueError(f"{call}: q contiguous [R,Hq,d], block_table [R,max_blocks]")
+    R, Hq, d = q.shape
+    pages, Hk = _cache_args(call, cache, d, page_size)
+    _int32(call, "block_table", block_table, (R, block_table.shape[1]))
+    _int32(call, "lens", lens, (R,))
+    blocks = block_table.shape[1]
+    if max_len is None:
+        max_len = blocks * page_size
+    O = torch.empty((R, Hq, d), dtype=torch.float32, device=dev)
+    tau = torch.empty((R, Hq), dtype=torch.float32, device=dev)
+    support = torch.empty((R, Hq), dtype=torch.int32, device=dev)
+    ws = workspace if workspace is not None else _workspace(entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len), dev)
+    with _Launch(dev) as stream:
+        _check(lib().entmax_attn_decode_cache4(_ptr(q), _ptr(cache), _ptr(block_table), _ptr(lens), _ptr(O), _ptr(tau), _ptr(support),
+                                               R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, float(alpha),
+                                               _ptr(ws), ws.numel() * ws.element_size(), stream))
+    return O, tau, support
 
 
 def entmax_attn_mfma_probe(data, sink, groups, iters):

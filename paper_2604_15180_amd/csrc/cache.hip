@@ -1,0 +1,349 @@
+// The paged 4-bit cache of a serving program: block tables and slots made on the GPU, rows written to their slots and
+// read back (layout: cache4.hpp).
+#include <limits.h>
+#include <math.h>
+
+#include "cache4.hpp"
+#include "common.hpp"
+#include "launch.hpp"
+
+namespace ea {
+
+// ---- block tables ---------------------------------------------------------------------------------------------------
+// One step of a scheduler: request r goes from lens[r] cached tokens to new_lens[r].  Pages that shrinking requests leave
+// go back to the top of the stack of free pages, the last request's last page first; growing requests then take theirs
+// from its top in their order.  A step taken back thus leaves the stack as it was.
+// Three prefix sums over the requests (pages left, pages wanted, new tokens) turn the work into independent items - a
+// page, a token row - that find their request by bisection.  Bound: latency, of the chain lengths -> sums -> stack ->
+// table -> slots; one work-group does all of it, so that its steps are a barrier apart and not a launch; the rows of a
+// long prompt are left to a second kernel with a work-group per 1024.
+
+constexpr int TABLE_MAX_REQUESTS = 4096;
+constexpr int TABLE_ROWS_INSIDE = 4096;         // token rows up to which the work-group of the tables makes the slots as well
+
+struct TableParams {
+    const int32_t* lens; const int32_t* new_lens;
+    int32_t* table;            // [R][blocks]
+    int32_t* free_pages;       // [n_pages]
+    int32_t* free_count;       // [1]
+    int32_t* lens_out;         // [R]
+    int32_t* start;            // [R + 1]
+    int32_t* slots; int32_t* positions;     // [rows]
+    int32_t* status;           // [4]
+    int R, blocks, page_shift, n_pages, rows;
+};
+
+EA_DEV int pages_of(int len, int shift) { return (len + (1 << shift) - 1) >> shift; }
+
+// largest r with pref[r] <= i, for i < pref[R] (so that request r has an item i)
+EA_DEV int owner(const int32_t* pref, int R, int i) {
+    int lo = 0, hi = R;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pref[mid] <= i) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// slot and position of token row t; `start`, `lens_out` and the table are final
+EA_DEV void table_row(const TableParams& p, const int32_t* start, int t) {
+    int slot = -1, position = 0;
+    if (t < start[p.R]) {
+        const int r = owner(start, p.R, t);
+        const int after = p.new_lens[r], old = after - (start[r + 1] - start[r]);
+        position = old + (t - start[r]);
+        if (p.lens_out[r] == after) {
+            const int page = p.table[(long)r * p.blocks + (position >> p.page_shift)];
+            if ((unsigned)page < (unsigned)p.n_pages) slot = (page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
+        }
+    }
+    p.slots[t] = slot;
+    p.positions[t] = position;
+}
+
+__global__ __launch_bounds__(1024) void cache_tables_kernel(TableParams p) {
+    constexpr int T = 1024, NW = T / 64;
+    __shared__ int32_t left[TABLE_MAX_REQUESTS + 1], want[TABLE_MAX_REQUESTS + 1], start[TABLE_MAX_REQUESTS + 1];   // exclusive prefix sums
+    __shared__ long long wsum[NW][3];
+    __shared__ int refused, invalid, strange, given;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = p.R;
+    const int most = (int)min((long long)p.blocks << p.page_shift, (long long)INT_MAX);
+    const int count = min(max(*p.free_count, 0), p.n_pages);
+    if (tid == 0) { refused = invalid = strange = given = 0; left[0] = want[0] = start[0] = 0; }
+    // a request whose lengths are out of range takes part in nothing
+    auto lengths = [&](int r, int& a, int& b) {
+        a = p.lens[r]; b = p.new_lens[r];
+        const bool ok = a >= 0 && b >= 0 && a <= most && b <= most;
+        if (!ok) a = b = 0;
+        return ok;
+    };
+    long long before[3] = {0, 0, 0};
+    for (int r0 = 0; r0 < R; r0 += T) {
+        const int r = r0 + tid;
+        long long v[3] = {0, 0, 0};
+        int a = 0, b = 0;
+        const bool ok = r >= R || lengths(r, a, b);
+        const int have = pages_of(a, p.page_shift), need = pages_of(b, p.page_shift);
+        v[0] = max(have - need, 0); v[1] = max(need - have, 0); v[2] = max(b - a, 0);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const long long up = __shfl_up(v[k], off);
+                if (lane >= off) v[k] += up;
+            }
+        }
+        __syncthreads();                                  // (of the round before: the sums have been read)
+        if (lane == 63) { wsum[wave][0] = v[0]; wsum[wave][1] = v[1]; wsum[wave][2] = v[2]; }
+        if (!ok) atomicAdd(&invalid, 1);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            long long all = 0;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                if (w < wave) v[k] += wsum[w][k];
+                all += wsum[w][k];
+            }
+            v[k] += before[k];
+            before[k] += all;
+        }
+        // (tokens: what does not fit 31 bits fits no list of rows either)
+        if (r < R) { left[r + 1] = (int)v[0]; want[r + 1] = (int)v[1]; start[r + 1] = (int)min(v[2], (long long)INT_MAX); }
+    }
+    __syncthreads();
+    const int back = left[R];
+    for (int i = tid; i < back; i += T) {
+        const int r = owner(left, R, i);
+        const int b = pages_of(p.new_lens[r], p.page_shift) + (i - left[r]);
+        const int at = count + (back - 1 - i), page = p.table[(long)r * p.blocks + b];
+        if (at < p.n_pages) p.free_pages[at] = page;
+        if (at >= p.n_pages || (unsigned)page >= (unsigned)p.n_pages) atomicAdd(&strange, 1);
+    }
+    __syncthreads();
+    const int top = min(count + back, p.n_pages);
+    for (int r = tid; r < R; r += T) {
+        int a, b;
+        const bool ok = lengths(r, a, b);
+        const bool wants = want[r + 1] > want[r], grows = b > a;
+        const bool fits = (!wants || want[r + 1] <= top) && (!grows || start[r + 1] <= p.rows);
+        if (!fits) atomicAdd(&refused, 1);
+        else if (wants) atomicMax(&given, want[r + 1]);
+        p.start[r + 1] = start[r + 1];
+        const int old = p.lens[r];
+        p.lens_out[r] = ok && fits ? b : old;             // (lens may be lens_out: each thread has read its own)
+    }
+    if (tid == 0) p.start[0] = 0;
+    __syncthreads();
+    // (the requests that get pages are the first ones that want any: both conditions only grow)
+    const int g = given;
+    for (int i = tid; i < g; i += T) {
+        const int r = owner(want, R, i);
+        const int old = p.new_lens[r] - (start[r + 1] - start[r]);
+        const int page = p.free_pages[top - 1 - i];
+        if ((unsigned)page >= (unsigned)p.n_pages) atomicAdd(&strange, 1);
+        p.table[(long)r * p.blocks + pages_of(old, p.page_shift) + (i - want[r])] = page;
+    }
+    if (tid == 0) *p.free_count = top - g;
+    __syncthreads();
+    if (tid == 0) { p.status[0] = min(start[R], p.rows); p.status[1] = refused; p.status[2] = invalid; p.status[3] = strange; }
+    if (p.rows <= TABLE_ROWS_INSIDE)
+        for (int t = tid; t < p.rows; t += T) table_row(p, start, t);
+}
+
+__global__ __launch_bounds__(256) void cache_slots_kernel(TableParams p) {
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t < p.rows) table_row(p, p.start, t);
+}
+
+// ---- rows in 4 bits -------------------------------------------------------------------------------------------------
+// A block of 32 values is four lanes with eight each.  Scale 2^s with s = floor(log2 max|x|) - 2, one more where
+// max|x| > 7 * 2^s: then no value is further from its level than half the distance of two levels, 6 and the
+// next power of two among them (with s alone, values up to 8 * 2^s would be cut to 6 * 2^s).  The scale is a power of two, so
+// x / 2^s is exact and the rounding to a level, ties to the even code, is the only one.
+// Bound: HBM, 2 bytes (bf16) and 17/32 byte a value.
+
+struct RowParams {
+    const void* src[2]; void* dst[2];       // K, V (write: src, read: dst), strides st
+    long st[2][2];                          // token, head
+    unsigned char* cache;
+    const int32_t* slots;
+    int T, Hk, page_shift, n_pages;
+};
+
+template <int D> EA_DEV unsigned char* row_base(const RowParams& p, int slot, int h, int which, int& row) {
+    const int page = slot >> p.page_shift;
+    row = slot & ((1 << p.page_shift) - 1);
+    const long head = (long)page * p.Hk + h;
+    return p.cache + ((head * (2 * (D / 2 + D / 32)) + which * (D / 2 + D / 32)) << p.page_shift);
+}
+
+template <class E, int D>
+__global__ __launch_bounds__(256) void cache4_write_kernel(RowParams p) {
+    using elem = typename E::elem;
+    typedef elem vec __attribute__((ext_vector_type(8)));
+    constexpr int LPR = D / 8;
+    const long item = (long)blockIdx.x * 256 + threadIdx.x;
+    const int sub = (int)(item % LPR);
+    const long rowid = item / LPR;                          // [T][2][Hk]
+    const int per = 2 * p.Hk;
+    const long t = rowid / per;
+    if (t >= p.T) return;
+    const int which = (int)(rowid - t * per) >= p.Hk, h = (int)(rowid - t * per) - which * p.Hk;
+    const int slot = p.slots[t];
+    if (slot < 0 || (slot >> p.page_shift) >= p.n_pages) return;
+    const vec x = *(const vec*)((const elem*)p.src[which] + t * p.st[which][0] + h * p.st[which][1] + 8 * sub);
+    // magnitudes as integers: they order like the values, and infinities and NaN stay above all others
+    unsigned int top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint((float)x[e]) & 0x7fffffffu);
+    top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));     // over the block's four lanes
+    top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));
+    int byte = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u);                // (7 * 2^s has the fraction 0.75)
+    byte = min(max(byte, 1), 252);
+    const float scale = __uint_as_float((unsigned int)byte << 23);
+    unsigned int codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[0], (float)x[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[2], (float)x[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[4], (float)x[5], scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[6], (float)x[7], scale, 3);
+    if (top >= 0x7f800000u) { byte = 255; codes = 0; }
+    int row;
+    unsigned char* base = row_base<D>(p, slot, h, which, row);
+    *(unsigned int*)(base + row * (D / 2) + 4 * sub) = codes;
+    if ((sub & 3) == 0) base[((D / 2) << p.page_shift) + row * (D / 32) + (sub >> 2)] = (unsigned char)byte;
+}
+
+template <class E, int D>
+__global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p) {
+    using elem = typename E::elem;
+    typedef elem vec __attribute__((ext_vector_type(8)));
+    constexpr int LPR = D / 8;
+    const long item = (long)blockIdx.x * 256 + threadIdx.x;
+    const int sub = (int)(item % LPR);
+    const long rowid = item / LPR;
+    const int per = 2 * p.Hk;
+    const long t = rowid / per;
+    if (t >= p.T) return;
+    const int which = (int)(rowid - t * per) >= p.Hk, h = (int)(rowid - t * per) - which * p.Hk;
+    const int slot = p.slots[t];
+    if (slot < 0 || (slot >> p.page_shift) >= p.n_pages) return;
+    int row;
+    const unsigned char* base = row_base<D>(p, slot, h, which, row);
+    const unsigned int codes = *(const unsigned int*)(base + row * (D / 2) + 4 * sub);
+    const unsigned int byte = base[((D / 2) << p.page_shift) + row * (D / 32) + (sub >> 2)];
+    // 2^-127 is no normal number: byte 0, which no write leaves, is read through 2^-126 and halved
+    const float scale = byte == 255u ? __builtin_nanf("") : __uint_as_float(max(byte, 1u) << 23);
+    const float half = byte == 0u ? 0.5f : 1.f;
+    vec y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const unsigned int c = codes >> (4 * e);
+        const unsigned int m = c & 7u;
+        // level of three bits: two of exponent, one of fraction; 0.5 and 0 below
+        const float level = m < 2u ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
+        y[e] = (elem)(((c & 8u) ? -level : level) * scale * half);
+    }
+    *(vec*)((elem*)p.dst[which] + t * p.st[which][0] + h * p.st[which][1] + 8 * sub) = y;
+}
+
+}  // namespace ea
+
+namespace {
+using namespace ea;
+
+int cache_launched() {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
+    return EA_OK;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+bool cache_shape_ok(int Hk, int d, int page, long n_pages) {
+    return Hk > 0 && Hk <= 65535 && (d == 64 || d == 128) && cache_page_ok(page) && n_pages > 0 && n_pages * page <= (long)INT_MAX;
+}
+
+int rows_check(const void* k, const void* v, const int64_t* ks, const int64_t* vs, const int32_t* slots, const void* cache,
+               int T, int Hk, int d, int t, int n_pages, int page, bool writes_rows) {
+    if (!cache || !ks || !vs || (T > 0 && (!k || !v || !slots))) return EA_ERR_NULL;
+    if (t != EA_F32 && t != EA_BF16) return EA_ERR_DTYPE;
+    if (T < 0 || !cache_shape_ok(Hk, d, page, n_pages) || (long)T * 2 * Hk * (d / 8) > 0xffffff00l) return EA_ERR_SHAPE;   // (a launch holds 2^32 threads)
+    const int size = t == EA_BF16 ? 2 : 4;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(cache)) return EA_ERR_LAYOUT;
+    const int64_t* both[2] = {ks, vs};
+    for (const int64_t* st : both) {
+        if (st[0] < 0 || st[1] < 0 || (st[0] * size) % 16 || (st[1] * size) % 16) return EA_ERR_LAYOUT;
+        if (!writes_rows) continue;
+        // rows that are written must not overlap
+        const int64_t a = st[0], b = st[1];
+        const bool ok = (T <= 1 || a >= (b < a && Hk > 1 ? b * (Hk - 1) + d : d)) && (Hk == 1 || b >= (a <= b && T > 1 ? a * (T - 1) + d : d));
+        if (!ok) return EA_ERR_LAYOUT;
+    }
+    return EA_OK;
+}
+
+RowParams row_params(void* cache, const int32_t* slots, const int64_t* ks, const int64_t* vs, int T, int Hk, int page, int n_pages) {
+    RowParams p{};
+    p.cache = (unsigned char*)cache; p.slots = slots;
+    for (int i = 0; i < 2; ++i) { p.st[0][i] = ks[i]; p.st[1][i] = vs[i]; }
+    p.T = T; p.Hk = Hk; p.page_shift = cache_page_shift(page); p.n_pages = n_pages;
+    return p;
+}
+unsigned int row_groups(int T, int Hk, int d) { return (unsigned int)(((long)T * 2 * Hk * (d / 8) + 255) / 256); }
+
+}  // namespace
+
+extern "C" {
+
+int entmax_attn_cache_tables(const int32_t* lens, const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
+                             int32_t* free_count, int32_t* lens_out, int32_t* token_start, int32_t* slots, int32_t* positions,
+                             int32_t* status, int R, int max_blocks, int page_size, int n_pages, int max_tokens, void* hip_stream) {
+    if (!lens || !new_lens || !block_table || !free_pages || !free_count || !lens_out || !token_start || !status) return EA_ERR_NULL;
+    if (max_tokens > 0 && (!slots || !positions)) return EA_ERR_NULL;
+    if (R <= 0 || R > TABLE_MAX_REQUESTS || max_blocks <= 0 || !cache_page_ok(page_size) || n_pages <= 0 || max_tokens < 0 || max_tokens > (1 << 30))
+        return EA_ERR_SHAPE;
+    if ((long)max_blocks * page_size > (1l << 22) || (long)n_pages * page_size > (long)INT_MAX) return EA_ERR_SHAPE;
+    if (lens_out == new_lens) return EA_ERR_LAYOUT;
+    TableParams p{lens, new_lens, block_table, free_pages, free_count, lens_out, token_start, slots, positions, status,
+                  R, max_blocks, cache_page_shift(page_size), n_pages, max_tokens};
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipLaunchKernelGGL(cache_tables_kernel, dim3(1), dim3(1024), 0, s, p);
+    if (max_tokens > TABLE_ROWS_INSIDE) hipLaunchKernelGGL(cache_slots_kernel, dim3((max_tokens + 255) / 256), dim3(256), 0, s, p);
+    return cache_launched();
+}
+
+size_t entmax_attn_cache4_page_bytes(int Hk, int d, int page_size) {
+    if (!cache_shape_ok(Hk, d, page_size, 1)) return 0;
+    return (size_t)Hk * cache_page_bytes(d, page_size);
+}
+
+int entmax_attn_cache4_write(const void* K, const void* V, const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                             void* cache, int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream) {
+    const int rc = rows_check(K, V, k_strides, v_strides, slots, cache, T, Hk, d, dtype, n_pages, page_size, false);
+    if (rc) return rc;
+    if (T == 0) return EA_OK;
+    RowParams p = row_params(cache, slots, k_strides, v_strides, T, Hk, page_size, n_pages);
+    p.src[0] = K; p.src[1] = V;
+    const dim3 grid(row_groups(T, Hk, d));
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (dtype == EA_BF16) { if (d == 64) hipLaunchKernelGGL((cache4_write_kernel<Bf16, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_write_kernel<Bf16, 128>), grid, dim3(256), 0, s, p); }
+    else { if (d == 64) hipLaunchKernelGGL((cache4_write_kernel<F32, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_write_kernel<F32, 128>), grid, dim3(256), 0, s, p); }
+    return cache_launched();
+}
+
+int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
+                            int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream) {
+    const int rc = rows_check(K, V, k_strides, v_strides, slots, cache, T, Hk, d, dtype, n_pages, page_size, true);
+    if (rc) return rc;
+    if (T == 0) return EA_OK;
+    RowParams p = row_params(const_cast<void*>(cache), slots, k_strides, v_strides, T, Hk, page_size, n_pages);
+    p.dst[0] = K; p.dst[1] = V;
+    const dim3 grid(row_groups(T, Hk, d));
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (dtype == EA_BF16) { if (d == 64) hipLaunchKernelGGL((cache4_read_kernel<Bf16, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_read_kernel<Bf16, 128>), grid, dim3(256), 0, s, p); }
+    else { if (d == 64) hipLaunchKernelGGL((cache4_read_kernel<F32, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_read_kernel<F32, 128>), grid, dim3(256), 0, s, p); }
+    return cache_launched();
+}
+
+}  // extern "C"
