@@ -324,9 +324,9 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  * A request of length 0 gets O = 0, tau = 0, support 0.  One whose length is negative or above max_len, or that has a
  * page id outside 0 .. n_pages - 1 among the pages it attends to, gets NaN and support -1, and so does a head with a score
  * that is infinite or NaN.  What the cache holds behind a request's last token has no effect.
- * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or four (float32) 8-bit terms: a bf16
- * element is exact down to 2^-13 of the largest of its row and known to 2^-21 of that below, a float32 element
- * to 2^-26 of it (rows whose largest element is below 2^-100 lose more); the rest is in float32.
+ * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or five (float32) 8-bit terms: a bf16
+ * element is exact down to 2^-12 of the largest of its row and known to 2^-20 of that below, a float32 element is exact down to
+ * 2^-6 and known to 2^-30 (rows whose largest element is below 2^-100 lose more); the rest is in float32.
  * Results repeat bit for bit.  Two calls at once need two workspaces.
  */
 size_t entmax_attn_cache4_page_bytes(int Hk, int d, int page_size);      /* 0 for a bad shape */

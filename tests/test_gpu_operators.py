@@ -356,8 +356,8 @@ def check_decode(q, ks, vs, alpha, O, tau, support, dtype):
         qi = q[i].double().numpy()[None]
         want = eo.attn_decode(qi, K, V, alpha)
         c = (alpha - 1) / np.sqrt(d)
-        small = np.abs(qi) < np.abs(qi).max(-1, keepdims=True) * 2.0 ** (-13 if dtype == "bf16" else -2)
-        lost = np.abs(qi).max(-1, keepdims=True) * (2.0 ** -21 if dtype == "bf16" else 2.0 ** -26) * small
+        small = np.abs(qi) < np.abs(qi).max(-1, keepdims=True) * 2.0 ** (-12 if dtype == "bf16" else -6)
+        lost = np.abs(qi).max(-1, keepdims=True) * (2.0 ** -20 if dtype == "bf16" else 2.0 ** -30) * small
         ds = d * U * (np.abs(K) @ np.abs(qi)[..., None])[..., 0] + (np.abs(K) @ lost[..., None])[..., 0]
         eta = 2 * c * ds.max(-1, keepdims=True) + 4 * U + 2e-6 * max(1.0, r / 4)
         x = (alpha - 1) * want["z"] - want["tau"][..., None]

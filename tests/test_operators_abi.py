@@ -119,7 +119,7 @@ def test_decode_refusals(L):
     assert decode(L, q=A + 8) == LAYOUT and decode(L, cache=A + 8) == LAYOUT
     assert decode(L, ws=None) == WORKSPACE and decode(L, ws=A + 128) == WORKSPACE and decode(L, nbytes=100) == WORKSPACE
     f = ea.entmax_attn_decode_cache4_workspace_bytes
-    assert f(1, 32, 8, 128, 1000) >= 32 * 1000 * 8 and f(1, 32, 7, 128, 1000) == 0 and f(1, 32, 8, 128, 0) == 0
+    assert f(1, 32, 8, 128, 1000) >= 32 * 1000 * 4 and f(1, 32, 7, 128, 1000) == 0 and f(1, 32, 8, 128, 0) == 0
 
 
 def test_bindings_refuse_cpu_tensors_and_wrong_types():
