@@ -291,46 +291,51 @@ def entmax_attn_decode(q, K, V, alpha, workspace=None):
 
 # ---- queries and keys from a layer's projections; the 4-bit cache --------------------------------
 
-def _on_gpu(call, *tensors):
-    """The one device of the tensors (None is skipped), made current for the launch by the caller's `with`."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{call}: tensors must live on the GPU (there is no CPU path)")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{call}: tensors on {dev} and {t.device}")
+# These calls are made once a layer and token in a serving program, where a kernel takes a few microseconds: what the binding does
+# around the library's call counts.  Devices are compared as integers, pointers passed as integers, and the stream is asked for without
+# making a Stream object (entmax_attn_cache_tables: 14.6 -> 11.4 us of host time a call,
+# of which the launch is 3).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on_gpu(call, first, *others):
+    """Index of the one device of the tensors (None is skipped)."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError(f"{call}: tensors must live on the GPU (there is no CPU path)")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            if not t.is_cuda:
+                raise ValueError(f"{call}: tensors must live on the GPU (there is no CPU path)")
+            raise ValueError(f"{call}: tensors on GPU {dev} and GPU {t.get_device()}")
     return dev
 
 
-class _Launch:
-    """Launches go to the current stream of the tensors' device, with that device current."""
-    __slots__ = ("dev", "before")
+def _launch(dev, function, *args):
+    """Calls the library with `args` and the current stream of device `dev`, with that device current."""
+    before = torch.cuda.current_device()
+    if before == dev:
+        rc = function(*args, _raw_stream(dev))
+    else:
+        torch.cuda.set_device(dev)
+        try:
+            rc = function(*args, _raw_stream(dev))
+        finally:
+            torch.cuda.set_device(before)
+    if rc:
+        _check(rc)
 
-    def __init__(self, dev):
-        self.dev = dev.index
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.dev:
-            torch.cuda.set_device(self.dev)
-        return torch.cuda.current_stream(self.dev).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.dev:
-            torch.cuda.set_device(self.before)
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _int32(call, name, t, shape):
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{call}: {name} must be contiguous int32 {list(shape)}, got {t.dtype} {list(t.shape)}")
 
 
-def _strides(*n):
-    return (ctypes.c_int64 * len(n))(*n)
+_TwoStrides, _ThreeStrides = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
 def _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections):
@@ -351,7 +356,7 @@ def _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sectio
         if sections is not None and len(sections) != axes:
             raise ValueError(f"{call}: {len(sections)} sections for {axes} position axes")
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
+        if w is not None and (w.dtype != torch.float32 or w.shape != (d,) or not w.is_contiguous()):
             raise ValueError(f"{call}: a weight must be contiguous float32 [{d}]")
     if not norm and (q_weight is not None or k_weight is not None):
         raise ValueError(f"{call}: weights go with norm=True")
@@ -360,7 +365,7 @@ def _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sectio
 
 
 def _row_strides(t):
-    return _strides(t.stride(0), t.stride(1), t.stride(2))
+    return _ThreeStrides(*t.stride()[:3])
 
 
 def entmax_attn_qk_norm_rope_fwd(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, norm=True, sections=None,
@@ -371,13 +376,10 @@ def entmax_attn_qk_norm_rope_fwd(q, k, positions, inv_freq, q_weight=None, k_wei
     call = "entmax_attn_qk_norm_rope_fwd"
     dev = _on_gpu(call, q, k, positions, inv_freq, q_weight, k_weight)
     B, N, Hq, Hk, d, rot, axes, sec = _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections)
-    q_out = torch.empty((B, Hq, N, d), dtype=q.dtype, device=dev)
-    k_out = torch.empty((B, Hk, N, d), dtype=q.dtype, device=dev)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_qk_norm_rope_fwd(
-            _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _row_strides(q), _row_strides(k), _ptr(q_weight), _ptr(k_weight),
-            _ptr(positions), _ptr(inv_freq), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, int(bool(interleaved)),
-            int(bool(norm)), float(eps), stream))
+    q_out, k_out = q.new_empty((B, Hq, N, d)), q.new_empty((B, Hk, N, d))
+    _launch(dev, lib().entmax_attn_qk_norm_rope_fwd, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _row_strides(q),
+            _row_strides(k), _at(q_weight), _at(k_weight), _at(positions), _at(inv_freq), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes,
+            sec, bool(interleaved), bool(norm), eps)
     return q_out, k_out
 
 
@@ -394,24 +396,22 @@ def entmax_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_we
     dev = _on_gpu(call, q, k, dq_out, dk_out, positions, inv_freq, q_weight, k_weight, workspace, *(out or ()))
     B, N, Hq, Hk, d, rot, axes, sec = _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections)
     for g, H in ((dq_out, Hq), (dk_out, Hk)):
-        if g.dtype != torch.float32 or tuple(g.shape) != (B, H, N, d) or not g.is_contiguous():
+        if g.dtype != torch.float32 or g.shape != (B, H, N, d) or not g.is_contiguous():
             raise ValueError(f"{call}: dq_out, dk_out must be contiguous float32 [B,H,N,d]")
     if out is None:
-        dq, dk = (torch.empty((B, N, H, d), dtype=q.dtype, device=dev) for H in (Hq, Hk))
+        dq, dk = q.new_empty((B, N, Hq, d)), q.new_empty((B, N, Hk, d))
     else:
         dq, dk = out
         if dq.shape != q.shape or dk.shape != k.shape or dq.dtype != q.dtype or dk.dtype != q.dtype or dq.stride(3) != 1 or dk.stride(3) != 1:
             raise ValueError(f"{call}: out must be of q's and k's shapes and dtype, rows contiguous")
-    dwq, dwk = (None if w is None else torch.empty(d, dtype=torch.float32, device=dev) for w in (q_weight, k_weight))
+    dwq, dwk = (None if w is None else w.new_empty(d) for w in (q_weight, k_weight))
     ws = workspace
     if ws is None and (dwq is not None or dwk is not None):
-        ws = _workspace(entmax_attn_qk_norm_rope_workspace_bytes(d), dev)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_qk_norm_rope_bwd(
-            _ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _row_strides(q), _row_strides(k), _row_strides(dq),
-            _row_strides(dk), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(inv_freq), _ptr(dwq), _ptr(dwk),
-            B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, int(bool(interleaved)), int(bool(norm)), float(eps),
-            _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), stream))
+        ws = _workspace(entmax_attn_qk_norm_rope_workspace_bytes(d), q.device)
+    _launch(dev, lib().entmax_attn_qk_norm_rope_bwd, q.data_ptr(), k.data_ptr(), dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(),
+            dk.data_ptr(), _row_strides(q), _row_strides(k), _row_strides(dq), _row_strides(dk), _at(q_weight), _at(k_weight),
+            _at(positions), _at(inv_freq), _at(dwq), _at(dwk), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, bool(interleaved),
+            bool(norm), eps, _at(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return dq, dk, dwq, dwk
 
 
@@ -429,15 +429,14 @@ def entmax_attn_cache_tables(lens, new_lens, block_table, free_pages, free_count
                            ("free_pages", free_pages, free_pages.shape), ("free_count", free_count, (1,))):
         _int32(call, name, t, shape)
     if out is None:
-        both = torch.empty(2 * R + 5 + 2 * max(max_tokens, 0), dtype=torch.int32, device=dev)
-        out = both.split([R, R + 1, max_tokens, max_tokens, 4]) if max_tokens >= 0 else (both,) * 5
+        if max_tokens < 0:
+            raise ValueError(f"{call}: max_tokens must not be negative")
+        out = torch.empty(2 * R + 5 + 2 * max_tokens, dtype=torch.int32, device=lens.device).split([R, R + 1, max_tokens, max_tokens, 4])
     else:
         for name, t, shape in zip(("lens_out", "token_start", "slots", "positions", "status"), out, shapes):
             _int32(call, name, t, shape)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_cache_tables(
-            _ptr(lens), _ptr(new_lens), _ptr(block_table), _ptr(free_pages), _ptr(free_count), *(_ptr(t) for t in out),
-            R, blocks, page_size, free_pages.numel(), max_tokens, stream))
+    _launch(dev, lib().entmax_attn_cache_tables, lens.data_ptr(), new_lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+            free_count.data_ptr(), *[t.data_ptr() for t in out], R, blocks, page_size, free_pages.numel(), max_tokens)
     return tuple(out)
 
 
@@ -465,7 +464,7 @@ def _cache_rows(call, k, v, slots, Hk):
     if k.numel() and (k.stride(2) != 1 or v.stride(2) != 1):
         raise ValueError(f"{call}: the elements of a row must be contiguous")
     _int32(call, "slots", slots, (k.shape[0],))
-    return _strides(k.stride(0), k.stride(1)), _strides(v.stride(0), v.stride(1))
+    return _TwoStrides(*k.stride()[:2]), _TwoStrides(*v.stride()[:2])
 
 
 def entmax_attn_cache4_write(K, V, slots, cache, page_size):
@@ -475,9 +474,8 @@ def entmax_attn_cache4_write(K, V, slots, cache, page_size):
     d = K.shape[-1]
     pages, Hk = _cache_args(call, cache, d, page_size)
     ks, vs = _cache_rows(call, K, V, slots, Hk)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_cache4_write(_ptr(K), _ptr(V), ks, vs, _ptr(slots), _ptr(cache), K.shape[0], Hk, d,
-                                              _dtype_code(K.dtype), pages, page_size, stream))
+    _launch(dev, lib().entmax_attn_cache4_write, K.data_ptr(), V.data_ptr(), ks, vs, slots.data_ptr(), cache.data_ptr(), K.shape[0], Hk, d,
+            _dtype_code(K.dtype), pages, page_size)
 
 
 def entmax_attn_cache4_read(cache, slots, page_size, d, dtype=torch.bfloat16, out=None):
@@ -487,14 +485,13 @@ def entmax_attn_cache4_read(cache, slots, page_size, d, dtype=torch.bfloat16, ou
     dev = _on_gpu(call, cache, slots, *(out or ()))
     pages, Hk = _cache_args(call, cache, d, page_size)
     if out is None:
-        out = tuple(torch.empty((slots.numel(), Hk, d), dtype=dtype, device=dev) for _ in range(2))
+        out = (cache.new_empty((slots.numel(), Hk, d), dtype=dtype), cache.new_empty((slots.numel(), Hk, d), dtype=dtype))
     K, V = out
     if K.shape[-1] != d:
         raise ValueError(f"{call}: out must be [T,Hk,{d}]")
     ks, vs = _cache_rows(call, K, V, slots, Hk)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_cache4_read(_ptr(cache), _ptr(slots), _ptr(K), _ptr(V), ks, vs, K.shape[0], Hk, d,
-                                             _dtype_code(K.dtype), pages, page_size, stream))
+    _launch(dev, lib().entmax_attn_cache4_read, cache.data_ptr(), slots.data_ptr(), K.data_ptr(), V.data_ptr(), ks, vs, K.shape[0], Hk, d,
+            _dtype_code(K.dtype), pages, page_size)
     return K, V
 
 
@@ -517,14 +514,11 @@ def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max
     blocks = block_table.shape[1]
     if max_len is None:
         max_len = blocks * page_size
-    O = torch.empty((R, Hq, d), dtype=torch.float32, device=dev)
-    tau = torch.empty((R, Hq), dtype=torch.float32, device=dev)
-    support = torch.empty((R, Hq), dtype=torch.int32, device=dev)
-    ws = workspace if workspace is not None else _workspace(entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len), dev)
-    with _Launch(dev) as stream:
-        _check(lib().entmax_attn_decode_cache4(_ptr(q), _ptr(cache), _ptr(block_table), _ptr(lens), _ptr(O), _ptr(tau), _ptr(support),
-                                               R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, float(alpha),
-                                               _ptr(ws), ws.numel() * ws.element_size(), stream))
+    O, tau, support = q.new_empty((R, Hq, d), dtype=torch.float32), q.new_empty((R, Hq), dtype=torch.float32), lens.new_empty((R, Hq))
+    ws = workspace if workspace is not None else _workspace(entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len), q.device)
+    _launch(dev, lib().entmax_attn_decode_cache4, q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), lens.data_ptr(), O.data_ptr(),
+            tau.data_ptr(), support.data_ptr(), R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, alpha,
+            ws.data_ptr(), ws.numel() * ws.element_size())
     return O, tau, support
 
 

@@ -49,28 +49,37 @@ struct Cache4Params {
 // 32 g .. 32 g + 31, whose scale byte is the lane's own; the scale of a column's block b is that of lane (n, b)).
 template <int NT> struct QTerms { i32x8 t[NT]; int scale[NT]; };
 
-// The waves of a work-group convert a quarter of the words each and hand them round through LDS.  Every thread calls this.
-template <class E, int D, int NT> EA_DEV void load_query(const void* q, long head, bool live, int wave, int (*words)[8][64], QTerms<NT>& out) {
+// What a lane reads of its head's row, 16 elements of each 64.
+template <class E, int D> struct QRow {
     using elem = typename E::elem;
     typedef elem vec __attribute__((ext_vector_type(8)));
-    constexpr int RUNS = D / 64, MINE = RUNS;             // words of four elements: 4 per run and lane, a quarter of them this wave's
-    const int lane = __lane_id(), g = lane >> 4;
-    float top = 0.f, x[MINE][4];
+    vec v[D / 64][2];
+    EA_DEV void load(const void* q, long head, bool live) {
+        const int g = __lane_id() >> 4;
+#pragma unroll
+        for (int run = 0; run < D / 64; ++run)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[run][half][e] = (elem)0.f;
+                if (live) v[run][half] = *(const vec*)((const elem*)q + head * D + 64 * run + 16 * g + 8 * half);
+            }
+    }
+};
+// The waves of a work-group convert a quarter of the words (of four elements) each and hand them round through LDS.  Every thread
+// calls this.
+template <class E, int D, int NT> EA_DEV void query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], QTerms<NT>& out) {
+    constexpr int RUNS = D / 64;
+    const int lane = __lane_id();
+    float top = 0.f, x[RUNS][4];
 #pragma unroll
     for (int run = 0; run < RUNS; ++run) {
-        vec v[2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[half][e] = (elem)0.f;
-            if (live) v[half] = *(const vec*)((const elem*)q + head * D + 64 * run + 16 * g + 8 * half);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)v[half][e]));
-        }
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf((float)row.v[run][0][e]), fabsf((float)row.v[run][1][e])));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float lo = (float)v[0][e], hi = (float)v[0][4 + e], lo2 = (float)v[1][e], hi2 = (float)v[1][4 + e];
-            x[run][e] = wave == 0 ? lo : wave == 1 ? hi : wave == 2 ? lo2 : hi2;
+            const auto &a = row.v[run][0], &b = row.v[run][1];
+            x[run][e] = (float)(wave == 0 ? a[e] : wave == 1 ? a[4 + e] : wave == 2 ? b[e] : b[4 + e]);
         }
     }
     top = fmaxf(top, __shfl_xor(top, 16));
@@ -125,32 +134,31 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
     // not fall on some of the XCDs, to which consecutive work-groups are dealt in turn (as the fastest index 48 requests took 98 us
     // where 28 us of keys are read: 16 parts a request put all their first parts on one XCD)
     const int kvh = blockIdx.x / p.colgroups, cg = blockIdx.x - kvh * p.colgroups, req = blockIdx.y, chunk = blockIdx.z;
-    const int len = p.lens[req];
-    if (len < 0 || len > p.max_len || chunk * C4_WAVES * p.part >= len) return;
+    const int shift = p.page_shift, in_page = (1 << shift) - 1;
+    const int k0 = (chunk * C4_WAVES + wave) * p.part, page0 = k0 >> shift;       // (at most C4_MAX_PART keys: 32 pages)
     const bool live = cg * 16 + n < p.G;
     const long head = (long)req * p.Hq + kvh * p.G + (live ? cg * 16 + n : 0);
-    const int k0 = (chunk * C4_WAVES + wave) * p.part, k1 = min(len, k0 + p.part);
+    // length, pages and query are asked for together, and the first keys before the query is worked on
+    const int len = p.lens[req];
+    int id = p.table[(long)req * p.blocks + min(page0 + lane, p.blocks - 1)];
+    QRow<E, D> qrow;
+    qrow.load(p.q, head, live);
+    if (len < 0 || len > p.max_len || chunk * C4_WAVES * p.part >= len) return;
+    const int k1 = min(len, k0 + p.part), last = (k1 - 1) >> shift;
     if (threadIdx.x < 16) smax[threadIdx.x] = c4_ordered(-INFINITY);
+    const bool strange = page0 + lane <= last && (unsigned)id >= (unsigned)p.n_pages;
+    if ((unsigned)id >= (unsigned)p.n_pages) id = 0;
+    const bool bad = __any(strange);
     QTerms<NT> q;
-    load_query<E, D, NT>(p.q, head, live, wave, words, q);
-    if (k0 >= k1) return;
     float lmax = -INFINITY;
     float* const scores = p.scores + head * p.stride;
     float* const bmax = p.bmax + head * (p.stride / C4_BLOCK);
-    const int32_t* pages = p.table + (long)req * p.blocks;
-    const int shift = p.page_shift, in_page = (1 << shift) - 1;
     const long page_bytes = (long)(2 * (ROW + SROW)) << shift;
     const unsigned char* const heads = p.cache + kvh * page_bytes;
     const long stride = page_bytes * p.Hk;
     // the operand row and block this lane loads
     const int lrow = n * ROW + 16 * (SETS == 2 ? g & 1 : g), lsrow = n * SROW + (SETS == 2 ? g & 1 : g);
     struct Batch { i32x4 a[U]; int sc[U]; };
-    const int page0 = k0 >> shift, last = (k1 - 1) >> shift;          // (at most C4_MAX_PART keys: 32 pages)
-    int id = 0;
-    if (page0 + lane <= last) id = pages[page0 + lane];
-    const bool strange = (unsigned)id >= (unsigned)p.n_pages;
-    if (strange) id = 0;
-    const bool bad = __any(strange);
     // (tiles past the end load rows of the last page)
     auto load = [&](Batch& x, int t0) {
 #pragma unroll
@@ -220,7 +228,8 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
         }
     };
     Batch x0, x1;
-    load(x0, k0);
+    if (k0 < k1) load(x0, k0);
+    query_terms<E, D, NT>(qrow, wave, words, q);
     for (int t0 = k0; t0 < k1; t0 += 2 * C4_BLOCK) {
         if (t0 + C4_BLOCK < k1) load(x1, t0 + C4_BLOCK);
         compute(x0, t0);
@@ -234,7 +243,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 // evaluation and of the output.
 template <int D, int AM, int NW>
 __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) {
-    constexpr int SEG = NW <= 4 ? 1024 : 512, ROW = D / 2, SROW = D / 32, LPR = D / 8, AT_ONCE = 64 / LPR, U = 4;
+    constexpr int SEG = 512, ROW = D / 2, SROW = D / 32, LPR = D / 8, AT_ONCE = 64 / LPR, U = 4;
     __shared__ float lx[NW][SEG];           // c (s - s_max), in the order of the keys; then the probabilities
     __shared__ int lj[NW][SEG];             // key; then its slot
     __shared__ float red[2][NW][2];
@@ -436,7 +445,7 @@ template <class E, int D>
 void cache4_run(const Cache4Params& p, hipStream_t s) {
     const int per_group = C4_WAVES * p.part;
     hipLaunchKernelGGL((cache4_scores_kernel<E, D>), dim3(p.Hk * p.colgroups, p.R, (p.max_len + per_group - 1) / per_group), dim3(64 * C4_WAVES), 0, s, p);
-    if ((long)p.R * p.Hq < 512) cache4_entmax<D, 16>(p, s); else cache4_entmax<D, 4>(p, s);
+    if ((long)p.R * p.Hq < 512) cache4_entmax<D, 8>(p, s); else cache4_entmax<D, 4>(p, s);
 }
 
 }  // namespace ea
