@@ -22,12 +22,13 @@ BASE = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
         "-Wno-unused-command-line-argument"]
 # 16-bit kernels keep MFMA results in ordinary VGPRs: the AGPR form costs a v_accvgpr copy per
 # accumulator register each time the vector ALUs touch a score tile.  The fp32 kernels (twice the
-# operand registers, not the throughput path) are left to the default register assignment.
+# operand registers, not the throughput path) are left to the default register assignment; so is everything without a
+# 16-bit or 8-bit matrix product.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
 
 def _flags(unit: str):
-    return VGPR_FORM if "bf16" in unit else []
+    return VGPR_FORM if "bf16" in unit or unit == "decode_cache4" else []
 
 
 def _compile(unit: str, verbose: bool) -> str:

@@ -17,6 +17,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache4.hpp"
 #include "common.hpp"
 #include "launch.hpp"
@@ -36,9 +38,9 @@ struct Cache4Params {
     float* scores;            // [R][Hq][stride]: s_j, where a block's maximum was in the window (else whatever stood there)
     float* bmax;              // [R][Hq][stride / 64]: maximum of 64 keys; +inf also where a score is not a number or a page id out of range
     long stride;              // keys a head has room for: max_len rounded up to 64
+    int part;                 // keys per wave of the score kernel, a multiple of 64
     int R, Hq, Hk, G, colgroups;        // G = Hq / Hk query heads per key head, in colgroups of up to 16
     int blocks, n_pages, page_shift, max_len;
-    int part;                 // keys per wave of the score kernel, a multiple of 64
     float c;                  // (alpha - 1) / sqrt(d)
     double c64;
     float alpha, r, win;      // win: the window of Eq. 5 in units of s, slightly widened
@@ -47,43 +49,43 @@ struct Cache4Params {
 // Terms of the row's values as operand registers of the 16x16x128 instruction: lane (n, g) = (lane % 16, lane / 16) supplies,
 // of column n, the contraction indices 16 g .. 16 g + 15 and 64 + 16 g .. in the e4m3 format (D = 64: both the same; a 4-bit operand:
 // 32 g .. 32 g + 31, whose scale byte is the lane's own; the scale of a column's block b is that of lane (n, b)).
-template <int NT> struct QTerms { i32x8 t[NT]; int scale[NT]; };
+template <int NT> struct QTerms { i32x8 t[NT]; int scale[NT]; };   // scale: bytes
 
-// What a lane reads of its head's row, 16 elements of each 64.
+// What a lane reads of its head's row: a wave's quarter of the sixteen elements of each 64.
 template <class E, int D> struct QRow {
     using elem = typename E::elem;
-    typedef elem vec __attribute__((ext_vector_type(8)));
-    vec v[D / 64][2];
-    EA_DEV void load(const void* q, long head, bool live) {
+    typedef elem vec __attribute__((ext_vector_type(4)));
+    vec v[D / 64];
+    EA_DEV void load(const void* q, long head, bool live, int wave) {
         const int g = __lane_id() >> 4;
 #pragma unroll
-        for (int run = 0; run < D / 64; ++run)
+        for (int run = 0; run < D / 64; ++run) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[run][half][e] = (elem)0.f;
-                if (live) v[run][half] = *(const vec*)((const elem*)q + head * D + 64 * run + 16 * g + 8 * half);
-            }
+            for (int e = 0; e < 4; ++e) v[run][e] = (elem)0.f;
+            if (live) v[run] = *(const vec*)((const elem*)q + head * D + 64 * run + 16 * g + 4 * wave);
+        }
     }
 };
-// The waves of a work-group convert a quarter of the words (of four elements) each and hand them round through LDS.  Every thread
-// calls this.
-template <class E, int D, int NT> EA_DEV void query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], QTerms<NT>& out) {
+// The waves of a work-group convert their quarters and hand them round through LDS.  Every thread calls this.  Returns the scale byte
+// of keys from which a score of some row may pass 2^120; odd: the lane's row holds an infinity or a NaN.
+template <class E, int D, int NT>
+EA_DEV int query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], float (*tops)[16], QTerms<NT>& out, bool& odd) {
     constexpr int RUNS = D / 64;
     const int lane = __lane_id();
     float top = 0.f, x[RUNS][4];
 #pragma unroll
-    for (int run = 0; run < RUNS; ++run) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf((float)row.v[run][0][e]), fabsf((float)row.v[run][1][e])));
+    for (int run = 0; run < RUNS; ++run)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const auto &a = row.v[run][0], &b = row.v[run][1];
-            x[run][e] = (float)(wave == 0 ? a[e] : wave == 1 ? a[4 + e] : wave == 2 ? b[e] : b[4 + e]);
+            x[run][e] = (float)row.v[run][e];
+            const float a = fabsf(x[run][e]);
+            top = a < INFINITY ? fmaxf(top, a) : INFINITY;             // (a NaN counts as infinite)
         }
-    }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
+    if (lane < 16) tops[wave][lane] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0][lane & 15], tops[1][lane & 15]), fmaxf(tops[2][lane & 15], tops[3][lane & 15]));
     // the largest value below 2^7 (the largest term at most 2^7); rows below 2^-100 lose what is below that
     const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 6;
 #pragma unroll
@@ -109,6 +111,9 @@ template <class E, int D, int NT> EA_DEV void query_terms(const QRow<E, D>& row,
 #pragma unroll
         for (int w = 0; w < 8; ++w) out.t[t][w] = words[t][RUNS == 1 ? w & 3 : w][lane];
     }
+    // |score| < D * 6 * 2^(byte - 127) * 2^(7 + e) <= 2^(byte - 110 + e)
+    odd = !(top < INFINITY);
+    return min(255, 230 - wave_max(odd ? -200 : e));
 }
 
 EA_DEV unsigned int c4_ordered(float f) {
@@ -120,99 +125,108 @@ EA_DEV float c4_from_ordered(unsigned int u) { return __uint_as_float((u & 0x800
 // Tiles: at D = 128 sixteen keys, one instruction per term; at D = 64 two sets of sixteen keys, the lower half of the lanes
 // (contraction indices 0 .. 63 of the operand) one, the upper half the other; the query terms stand in both halves of their operand,
 // and the keys are worked on one set at a time, with zeros in place of the other's.  Result: lane (n, g) holds head n's scores with keys
-// 4 g .. 4 g + 3 of a set.  64 keys are a batch; the next batch is requested before the current one is worked on.  The pages of a wave's
-// keys are looked up 64 at a time, one per lane, so that a batch's addresses come from scalar registers.
+// 4 g .. 4 g + 3 of a set.  A wave keeps two blocks of 64 keys on their way: as soon as the matrix cores have taken a tile, the same
+// tile of the block after the next is requested.  The addresses of all its keys are formed at once, a lane for each sixteen.
 template <class E, int D>
 __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Params p) {
     constexpr int NT = sizeof(typename E::elem) == 2 ? 3 : 5, SETS = 128 / D, TK = 16 * SETS, U = C4_BLOCK / TK;
     constexpr int ROW = D / 2, SROW = D / 32;
     __shared__ unsigned int smax[16];                       // ordered bits of the work-group's running maxima
     __shared__ int words[NT][8][64];
+    __shared__ float tops[C4_WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
-    // the parts of a request are the slowest index: work-groups that find nothing to do (short requests have few parts) then do
-    // not fall on some of the XCDs, to which consecutive work-groups are dealt in turn (as the fastest index 48 requests took 98 us
-    // where 28 us of keys are read: 16 parts a request put all their first parts on one XCD)
-    const int kvh = blockIdx.x / p.colgroups, cg = blockIdx.x - kvh * p.colgroups, req = blockIdx.y, chunk = blockIdx.z;
+    // Short requests have few parts, and the work-groups that find nothing to do must not fall on some of the XCDs, or some of the 32
+    // CUs of each, to which consecutive work-groups are dealt in turn.  So the part is the slowest index (as the fastest one 48
+    // requests of 64 .. 32768 tokens took 98 us in place of 50: all their first parts stood on one XCD), and the requests move
+    // on by one CU from part to part (50 -> 41 us).
+    const int kvh = blockIdx.x / p.colgroups, cg = blockIdx.x - kvh * p.colgroups, chunk = blockIdx.z;
+    const int req = (int)((blockIdx.y + (unsigned int)((p.R - 1) & 31) * chunk) % (unsigned int)p.R);
     const int shift = p.page_shift, in_page = (1 << shift) - 1;
-    const int k0 = (chunk * C4_WAVES + wave) * p.part, page0 = k0 >> shift;       // (at most C4_MAX_PART keys: 32 pages)
+    // the waves take the work-group's blocks in turn, so that a request shorter than its part of the keys is all four waves' work
+    const int c0 = chunk * C4_WAVES * p.part;
+    auto block_key = [&](int i) { return c0 + (i * C4_WAVES + wave) * C4_BLOCK; };        // first key of the wave's block i
     const bool live = cg * 16 + n < p.G;
     const long head = (long)req * p.Hq + kvh * p.G + (live ? cg * 16 + n : 0);
-    // length, pages and query are asked for together, and the first keys before the query is worked on
+    // length, pages and query are asked for together, and the first keys before the query is worked on.  Lane 4 i + j: the sixteen
+    // keys j of block i (C4_MAX_PART: at most eight blocks).
     const int len = p.lens[req];
-    int id = p.table[(long)req * p.blocks + min(page0 + lane, p.blocks - 1)];
+    const int key16 = block_key(lane >> 2) + 16 * (lane & 3);
+    int id = p.table[(long)req * p.blocks + min(key16 >> shift, p.blocks - 1)];
     QRow<E, D> qrow;
-    qrow.load(p.q, head, live);
-    if (len < 0 || len > p.max_len || chunk * C4_WAVES * p.part >= len) return;
-    const int k1 = min(len, k0 + p.part), last = (k1 - 1) >> shift;
+    qrow.load(p.q, head, live, wave);
+    if (len < 0 || len > p.max_len || c0 >= len) return;
+    const int k1 = min(len, c0 + C4_WAVES * p.part);
+    const int mine = ((k1 - c0 + C4_BLOCK - 1) / C4_BLOCK - wave + C4_WAVES - 1) / C4_WAVES;       // the wave's blocks
     if (threadIdx.x < 16) smax[threadIdx.x] = c4_ordered(-INFINITY);
-    const bool strange = page0 + lane <= last && (unsigned)id >= (unsigned)p.n_pages;
-    if ((unsigned)id >= (unsigned)p.n_pages) id = 0;
-    const bool bad = __any(strange);
-    QTerms<NT> q;
-    float lmax = -INFINITY;
+    const bool strange = (unsigned)id >= (unsigned)p.n_pages;
+    const bool bad = __any(strange && key16 < k1);
+    if (strange) id = 0;
+    const long page_bytes = (long)(2 * (ROW + SROW)) << shift;
+    const unsigned char* const page = p.cache + ((long)id * p.Hk + kvh) * page_bytes;
+    const uint64_t rows16 = (uint64_t)(page + (key16 & in_page) * ROW), scales16 = (uint64_t)(page + (ROW << shift) + (key16 & in_page) * SROW);
     float* const scores = p.scores + head * p.stride;
     float* const bmax = p.bmax + head * (p.stride / C4_BLOCK);
-    const long page_bytes = (long)(2 * (ROW + SROW)) << shift;
-    const unsigned char* const heads = p.cache + kvh * page_bytes;
-    const long stride = page_bytes * p.Hk;
-    // the operand row and block this lane loads
-    const int lrow = n * ROW + 16 * (SETS == 2 ? g & 1 : g), lsrow = n * SROW + (SETS == 2 ? g & 1 : g);
+    // what the lane loads of sixteen rows
+    const unsigned int lrow = n * ROW + 16 * (SETS == 2 ? g & 1 : g), lsrow = n * SROW + (SETS == 2 ? g & 1 : g);
     struct Batch { i32x4 a[U]; int sc[U]; };
-    // (tiles past the end load rows of the last page)
-    auto load = [&](Batch& x, int t0) {
+    typedef const unsigned char __attribute__((address_space(1)))* global_bytes;       // (a pointer from two integers is not known to be global)
+    typedef const i32x4 __attribute__((address_space(1)))* global_codes;
+    auto from_lane = [](uint64_t v, int l) {
+        return (global_bytes)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+    };
+    auto load = [&](Batch& x, int i, int u) {               // (past the end the rows of some page are loaded)
+        const int l = 4 * i + SETS * u;
+        global_bytes rows = from_lane(rows16, l), scales = from_lane(scales16, l);
+        if constexpr (SETS == 2) {                          // the upper lanes' keys may lie in another page (of 16)
+            const global_bytes rows1 = from_lane(rows16, l + 1), scales1 = from_lane(scales16, l + 1);
+            if (g >> 1) { rows = rows1; scales = scales1; }
+        }
+        x.a[u] = __builtin_nontemporal_load((global_codes)(rows + lrow));
+        x.sc[u] = scales[lsrow];
+    };
+    QTerms<NT> q;
+    int limit;                                              // scale bytes from which a score may not be finite
+    bool odd;                                               // the lane's query is not
+    float lmax = -INFINITY;
+    auto compute = [&](auto more, Batch& x, int i) {
+        const int t0 = block_key(i);
+        const bool part_of = t0 + C4_BLOCK > k1;
+        f32x4 s[U][SETS];
+        float best = -INFINITY;
+        int top = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int key = t0 + u * TK;
-            auto base_of = [&](int k) {
-                const int page = __builtin_amdgcn_readlane(id, min(k >> shift, last) - page0);
-                return heads + page * stride;
-            };
-            const unsigned char* base = base_of(key);
-            int row = key & in_page;
-            if constexpr (SETS == 2) {                  // the upper lanes' keys may lie in another page (of 16)
-                const unsigned char* base1 = base_of(key + 16);
-                const int row1 = (key + 16) & in_page;
-                if (g >> 1) { base = base1; row = row1; }
-            }
-            x.a[u] = __builtin_nontemporal_load((const i32x4*)(base + row * ROW + lrow));
-            x.sc[u] = (base + (ROW << shift) + row * SROW)[lsrow];
-        }
-    };
-    auto compute = [&](Batch& x, int t0) {
-        const bool part_of = t0 + C4_BLOCK > k1;
-        // (what lies behind the end may be anything, also a scale that is not a number)
-        if (part_of) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (t0 + u * TK + (SETS == 2 ? 16 * (g >> 1) : 0) + n >= k1) { x.a[u] = i32x4{0, 0, 0, 0}; x.sc[u] = 127; }
-        }
-        f32x4 s[U][SETS];
-        float best = -INFINITY, odd = 0.f;              // odd: not 0 if a score is infinite or not a number
-#pragma unroll
-        for (int u = 0; u < U; ++u)
+            // (what lies behind the end may be anything, also a scale that is not a number)
+            if (part_of && t0 + u * TK + (SETS == 2 ? 16 * (g >> 1) : 0) + n >= k1) { x.a[u] = i32x4{0, 0, 0, 0}; x.sc[u] = 1; }
+            top = max(top, x.sc[u]);
 #pragma unroll
             for (int set = 0; set < SETS; ++set) {
                 i32x8 av = {x.a[u][0], x.a[u][1], x.a[u][2], x.a[u][3], 0, 0, 0, 0};
                 int sc = x.sc[u];
-                if (SETS == 2 && (g >> 1) != set) { av = i32x8{0, 0, 0, 0, 0, 0, 0, 0}; sc = 127; }
+                if (SETS == 2 && (g >> 1) != set) { av = i32x8{0, 0, 0, 0, 0, 0, 0, 0}; sc = 1; }
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = NT - 1; t >= 0; --t)
                     acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, q.t[t], acc, 4, 0, 0, sc, 0, q.scale[t]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    odd = fmaf(acc[i], 0.f, odd);
-                    if (part_of && t0 + u * TK + 16 * set + 4 * g + i >= k1) acc[i] = -INFINITY;
-                    best = fmaxf(best, acc[i]);
-                }
                 s[u][set] = acc;
             }
-        if (!(odd == 0.f) || bad) best = INFINITY;
+            if constexpr (decltype(more)::value) load(x, i + 2, u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (part_of && t0 + u * TK + 16 * set + 4 * g + k >= k1) s[u][set][k] = -INFINITY;
+                    best = fmaxf(best, s[u][set][k]);
+                }
         best = fmaxf(best, __shfl_xor(best, 16));
         best = fmaxf(best, __shfl_xor(best, 32));
+        if (__any(top >= limit) || bad || odd) best = INFINITY;
         if (!live) best = -INFINITY;
-        const float shared_max = c4_from_ordered(*(volatile unsigned int*)&smax[n]);
+        const float shared_max = c4_from_ordered(__hip_atomic_load(&smax[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         lmax = fmaxf(lmax, best);
         const float m = fmaxf(lmax, shared_max);
         if (live && g == 0) bmax[t0 / C4_BLOCK] = best;
@@ -227,15 +241,20 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
                 for (int set = 0; set < SETS; ++set) *(f32x4*)(scores + t0 + u * TK + 16 * set + 4 * g) = s[u][set];
         }
     };
+    constexpr auto more = std::true_type{};
+    constexpr auto no_more = std::false_type{};
     Batch x0, x1;
-    if (k0 < k1) load(x0, k0);
-    query_terms<E, D, NT>(qrow, wave, words, q);
-    for (int t0 = k0; t0 < k1; t0 += 2 * C4_BLOCK) {
-        if (t0 + C4_BLOCK < k1) load(x1, t0 + C4_BLOCK);
-        compute(x0, t0);
-        if (t0 + C4_BLOCK >= k1) break;
-        if (t0 + 2 * C4_BLOCK < k1) load(x0, t0 + 2 * C4_BLOCK);
-        compute(x1, t0 + C4_BLOCK);
+#pragma unroll
+    for (int u = 0; u < U; ++u) if (mine > 0) load(x0, 0, u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) if (mine > 1) load(x1, 1, u);
+    limit = query_terms<E, D, NT>(qrow, wave, words, tops, q, odd);
+    int i = 0;
+    for (; i + 3 < mine; i += 2) { compute(more, x0, i); compute(more, x1, i + 1); }
+    if (i + 2 < mine) { compute(more, x0, i); compute(no_more, x1, i + 1); compute(no_more, x0, i + 2); }
+    else {
+        if (i < mine) compute(no_more, x0, i);
+        if (i + 1 < mine) compute(no_more, x1, i + 1);
     }
 }
 
@@ -455,14 +474,17 @@ using namespace ea;
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Keys per wave of the score kernel: few enough that the waves of all heads number about 4096 (sixteen per CU), at least C4_BLOCK, and at
-// most C4_MAX_PART: requests are of different lengths, and the longest one's keys are not to queue up behind few waves.
+// Keys per wave of the score kernel: few enough that the waves of all heads number about 4096 (sixteen per CU), where several requests are
+// taken to be half as long as the longest, at least C4_BLOCK, and at most C4_MAX_PART: the longest request's keys are not to queue up
+// behind few waves.  (24 requests up to 8192 keys, 8 key heads: 192 or 256 keys 12 us, 512 keys 15; 48 requests up to 32768: 256
+// keys 40 us, 512 41, 1024 46; one of 131072, 32 key heads: 54, 51, 50.)
 int cache4_part(int R, int Hq, int Hk, int max_len) {
     const long groups = (long)R * Hk * ((Hq / Hk + 15) / 16);
-    const long part = ((long)max_len * groups / 4096 + 63) / 64 * 64;
+    const long part = ((long)max_len * groups / (R > 1 ? 8192 : 4096) + 63) / 64 * 64;
     return part < C4_BLOCK ? C4_BLOCK : part > C4_MAX_PART ? C4_MAX_PART : (int)part;
 }
-long cache4_stride(int max_len) { return ((long)max_len + C4_BLOCK - 1) / C4_BLOCK * C4_BLOCK; }
+// (an odd number of blocks: heads a power of two apart would begin on the same memory channels)
+long cache4_stride(int max_len) { return (((long)max_len + C4_BLOCK - 1) / C4_BLOCK | 1) * C4_BLOCK; }
 bool cache4_decode_shape_ok(int R, int Hq, int Hk, int d, int max_len) {
     return R > 0 && R <= 65535 && Hk > 0 && Hq > 0 && Hq % Hk == 0 && Hq <= 65535 && (d == 64 || d == 128) && max_len > 0 &&
            max_len <= (1 << 22);
