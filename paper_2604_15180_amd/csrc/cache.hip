@@ -16,7 +16,8 @@ namespace ea {
 // Three prefix sums over the requests (pages left, pages wanted, new tokens) turn the work into independent items - a
 // page, a token row - that find their request by bisection.  Bound: latency, of the chain lengths -> sums -> stack ->
 // table -> slots; one work-group does all of it, so that its steps are a barrier apart and not a launch; the rows of a
-// long prompt are left to a second kernel with a work-group per 1024.
+// long prompt are left to a second kernel.  64 requests with a token each: 3.7 us; 1000 requests of which 150 end, start or go
+// back, with 61000 rows: 10.2 and 4.5 us (four pages a thread at once: 11.5).
 
 constexpr int TABLE_MAX_REQUESTS = 4096;
 constexpr int TABLE_ROWS_INSIDE = 4096;         // token rows up to which the work-group of the tables makes the slots as well
@@ -45,29 +46,38 @@ EA_DEV int owner(const int32_t* pref, int R, int i) {
     return lo;
 }
 
-// slot and position of token row t; `start`, `lens_out` and the table are final
-EA_DEV void table_row(const TableParams& p, const int32_t* start, int t) {
-    int slot = -1, position = 0;
-    if (t < start[p.R]) {
-        const int r = owner(start, p.R, t);
-        const int after = p.new_lens[r], old = after - (start[r + 1] - start[r]);
-        position = old + (t - start[r]);
-        if (p.lens_out[r] == after) {
-            const int page = p.table[(long)r * p.blocks + (position >> p.page_shift)];
-            if ((unsigned)page < (unsigned)p.n_pages) slot = (page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
-        }
+// position and slot of token row t of request r (the table is final)
+EA_DEV void table_row(const TableParams& p, int t, int r, int start, int end, bool granted) {
+    const int position = p.new_lens[r] - (end - start) + (t - start);
+    int slot = -1;
+    if (granted) {
+        const int page = p.table[(long)r * p.blocks + (position >> p.page_shift)];
+        if ((unsigned)page < (unsigned)p.n_pages) slot = (page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
     }
     p.slots[t] = slot;
     p.positions[t] = position;
 }
 
+// inclusive sum over the lanes up to this one, by data-parallel-primitive adds (through LDS each of the six steps waits for its
+// predecessor's round trip)
+template <int CTRL, int ROWS> EA_DEV int scan_step(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+EA_DEV int wave_scan(int v) {
+    v = scan_step<0x111, 0xf>(v);        // row_shr 1, 2, 4, 8: within sixteen lanes
+    v = scan_step<0x112, 0xf>(v);
+    v = scan_step<0x114, 0xf>(v);
+    v = scan_step<0x118, 0xf>(v);
+    v = scan_step<0x142, 0xa>(v);        // row_bcast 15: the row before, to the odd rows
+    v = scan_step<0x143, 0xc>(v);        // row_bcast 31: the lower half, to the upper one
+    return v;
+}
+
 __global__ __launch_bounds__(1024) void cache_tables_kernel(TableParams p) {
     constexpr int T = 1024, NW = T / 64;
     __shared__ int32_t left[TABLE_MAX_REQUESTS + 1], want[TABLE_MAX_REQUESTS + 1], start[TABLE_MAX_REQUESTS + 1];   // exclusive prefix sums
-    __shared__ long long wsum[NW][3];
+    __shared__ int32_t wsum[NW][4];
     __shared__ int refused, invalid, strange, given;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = p.R;
-    const int most = (int)min((long long)p.blocks << p.page_shift, (long long)INT_MAX);
+    const int most = p.blocks << p.page_shift;           // (at most 2^22)
     const int count = min(max(*p.free_count, 0), p.n_pages);
     if (tid == 0) { refused = invalid = strange = given = 0; left[0] = want[0] = start[0] = 0; }
     // a request whose lengths are out of range takes part in nothing
@@ -77,83 +87,78 @@ __global__ __launch_bounds__(1024) void cache_tables_kernel(TableParams p) {
         if (!ok) a = b = 0;
         return ok;
     };
-    long long before[3] = {0, 0, 0};
+    int a = 0, b = 0;                                     // of the thread's last request
+    bool ok = true;
+    long long tokens = 0;
+    int back = 0, wanted = 0;
     for (int r0 = 0; r0 < R; r0 += T) {
         const int r = r0 + tid;
-        long long v[3] = {0, 0, 0};
-        int a = 0, b = 0;
-        const bool ok = r >= R || lengths(r, a, b);
+        a = b = 0;
+        ok = r >= R || lengths(r, a, b);
         const int have = pages_of(a, p.page_shift), need = pages_of(b, p.page_shift);
-        v[0] = max(have - need, 0); v[1] = max(need - have, 0); v[2] = max(b - a, 0);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const long long up = __shfl_up(v[k], off);
-                if (lane >= off) v[k] += up;
-            }
-        }
+        // sums over a wave: pages below 2^24, tokens below 2^28
+        int v[3] = {wave_scan(max(have - need, 0)), wave_scan(max(need - have, 0)), wave_scan(max(b - a, 0))};
         __syncthreads();                                  // (of the round before: the sums have been read)
         if (lane == 63) { wsum[wave][0] = v[0]; wsum[wave][1] = v[1]; wsum[wave][2] = v[2]; }
         if (!ok) atomicAdd(&invalid, 1);
         __syncthreads();
+        long long at = tokens + v[2];
+        v[0] += back; v[1] += wanted;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            long long all = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                if (w < wave) v[k] += wsum[w][k];
-                all += wsum[w][k];
-            }
-            v[k] += before[k];
-            before[k] += all;
+        for (int w = 0; w < NW; ++w) {
+            const int s0 = wsum[w][0], s1 = wsum[w][1], s2 = wsum[w][2];
+            if (w < wave) { v[0] += s0; v[1] += s1; at += s2; }
+            back += s0; wanted += s1; tokens += s2;
         }
         // (tokens: what does not fit 31 bits fits no list of rows either)
-        if (r < R) { left[r + 1] = (int)v[0]; want[r + 1] = (int)v[1]; start[r + 1] = (int)min(v[2], (long long)INT_MAX); }
+        if (r < R) { left[r + 1] = v[0]; want[r + 1] = v[1]; start[r + 1] = (int)min(at, (long long)INT_MAX); }
     }
     __syncthreads();
-    const int back = left[R];
+    const int top = min(count + back, p.n_pages);
+    // request r is granted what it wants (both conditions only grow with r: the requests that get pages are the first that want any)
+    auto granted = [&](int r, bool grows) { return (want[r + 1] == want[r] || want[r + 1] <= top) && (!grows || start[r + 1] <= p.rows); };
+    for (int r = tid; r < R; r += T) {
+        if (R > T) ok = lengths(r, a, b);                 // (else still there)
+        const bool fits = granted(r, b > a);
+        if (!fits) atomicAdd(&refused, 1);
+        else if (want[r + 1] > want[r]) atomicMax(&given, want[r + 1]);
+        p.start[r + 1] = start[r + 1];
+        p.lens_out[r] = !ok ? p.lens[r] : fits ? b : a;   // (lens may be lens_out: each thread reads its own)
+    }
+    if (tid == 0) p.start[0] = 0;
     for (int i = tid; i < back; i += T) {
         const int r = owner(left, R, i);
-        const int b = pages_of(p.new_lens[r], p.page_shift) + (i - left[r]);
-        const int at = count + (back - 1 - i), page = p.table[(long)r * p.blocks + b];
+        const int k = pages_of(p.new_lens[r], p.page_shift) + (i - left[r]);
+        const int at = count + (back - 1 - i), page = p.table[(long)r * p.blocks + k];
         if (at < p.n_pages) p.free_pages[at] = page;
         if (at >= p.n_pages || (unsigned)page >= (unsigned)p.n_pages) atomicAdd(&strange, 1);
     }
     __syncthreads();
-    const int top = min(count + back, p.n_pages);
-    for (int r = tid; r < R; r += T) {
-        int a, b;
-        const bool ok = lengths(r, a, b);
-        const bool wants = want[r + 1] > want[r], grows = b > a;
-        const bool fits = (!wants || want[r + 1] <= top) && (!grows || start[r + 1] <= p.rows);
-        if (!fits) atomicAdd(&refused, 1);
-        else if (wants) atomicMax(&given, want[r + 1]);
-        p.start[r + 1] = start[r + 1];
-        const int old = p.lens[r];
-        p.lens_out[r] = ok && fits ? b : old;             // (lens may be lens_out: each thread has read its own)
-    }
-    if (tid == 0) p.start[0] = 0;
-    __syncthreads();
-    // (the requests that get pages are the first ones that want any: both conditions only grow)
     const int g = given;
     for (int i = tid; i < g; i += T) {
         const int r = owner(want, R, i);
-        const int old = p.new_lens[r] - (start[r + 1] - start[r]);
         const int page = p.free_pages[top - 1 - i];
+        const int old = p.new_lens[r] - (start[r + 1] - start[r]);
         if ((unsigned)page >= (unsigned)p.n_pages) atomicAdd(&strange, 1);
         p.table[(long)r * p.blocks + pages_of(old, p.page_shift) + (i - want[r])] = page;
     }
     if (tid == 0) *p.free_count = top - g;
     __syncthreads();
     if (tid == 0) { p.status[0] = min(start[R], p.rows); p.status[1] = refused; p.status[2] = invalid; p.status[3] = strange; }
-    if (p.rows <= TABLE_ROWS_INSIDE)
-        for (int t = tid; t < p.rows; t += T) table_row(p, start, t);
+    if (p.rows > TABLE_ROWS_INSIDE) return;               // (cache_slots_kernel)
+    for (int t = tid; t < p.rows; t += T) {
+        if (t < start[R]) { const int r = owner(start, R, t); table_row(p, t, r, start[r], start[r + 1], granted(r, true)); }
+        else { p.slots[t] = -1; p.positions[t] = 0; }
+    }
 }
 
 __global__ __launch_bounds__(256) void cache_slots_kernel(TableParams p) {
     const int t = blockIdx.x * 256 + threadIdx.x;
-    if (t < p.rows) table_row(p, p.start, t);
+    if (t >= p.rows) return;
+    if (t < p.start[p.R]) {
+        const int r = owner(p.start, p.R, t);
+        table_row(p, t, r, p.start[r], p.start[r + 1], p.lens_out[r] == p.new_lens[r]);
+    } else { p.slots[t] = -1; p.positions[t] = 0; }
 }
 
 // ---- rows in 4 bits -------------------------------------------------------------------------------------------------
@@ -161,7 +166,8 @@ __global__ __launch_bounds__(256) void cache_slots_kernel(TableParams p) {
 // max|x| > 7 * 2^s: then no value is further from its level than half the distance of two levels, 6 and the
 // next power of two among them (with s alone, values up to 8 * 2^s would be cut to 6 * 2^s).  The scale is a power of two, so
 // x / 2^s is exact and the rounding to a level, ties to the even code, is the only one.
-// Bound: HBM, 2 bytes (bf16) and 17/32 byte a value.
+// Bound: HBM, 2 bytes (bf16) and 17/32 byte a value: 16001 tokens of 16 rows of 128 values are written in 17.2 us and read back in
+// 17.0, 4.9 TB/s of reads and writes together (one item a thread: 18.0 and 19.5; 64 tokens 2.8 us, with four items a thread 4.1).
 
 struct RowParams {
     const void* src[2]; void* dst[2];       // K, V (write: src, read: dst), strides st
@@ -171,80 +177,100 @@ struct RowParams {
     int T, Hk, page_shift, n_pages;
 };
 
-template <int D> EA_DEV unsigned char* row_base(const RowParams& p, int slot, int h, int which, int& row) {
-    const int page = slot >> p.page_shift;
-    row = slot & ((1 << p.page_shift) - 1);
-    const long head = (long)page * p.Hk + h;
-    return p.cache + ((head * (2 * (D / 2 + D / 32)) + which * (D / 2 + D / 32)) << p.page_shift);
+constexpr unsigned int ROWS_MANY = 1u << 18;       // items from which a thread takes four (1024 work-groups of single ones)
+
+// An item is eight neighbouring values of a row; items of a token follow each other (K's heads, then V's).  Of a large batch each
+// thread takes U, a work-group's width apart, so that their loads are on their way together.
+struct RowItem { int t, which, h, sub, slot; bool on; };
+template <int D> EA_DEV RowItem row_item(const RowParams& p, unsigned int item, unsigned int items) {
+    constexpr unsigned int LPR = D / 8;
+    RowItem r;
+    const unsigned int id = min(item, items - 1) / LPR, per = 2u * p.Hk;
+    r.sub = (int)(item % LPR);
+    r.t = (int)(id / per);
+    const int i = (int)(id - r.t * per);
+    r.which = i >= p.Hk;
+    r.h = i - (r.which ? p.Hk : 0);
+    r.slot = p.slots[r.t];
+    r.on = item < items && r.slot >= 0 && (r.slot >> p.page_shift) < p.n_pages;
+    return r;
+}
+// Where the item's codes and its scale byte lie (the first page's for an item that takes no part)
+template <int D> EA_DEV void row_place(const RowParams& p, const RowItem& r, unsigned char*& codes, unsigned char*& scale) {
+    const int slot = r.on ? r.slot : 0;
+    const int row = slot & ((1 << p.page_shift) - 1);
+    const long head = (long)(slot >> p.page_shift) * p.Hk + r.h;
+    unsigned char* const base = p.cache + ((head * (2 * (D / 2 + D / 32)) + r.which * (D / 2 + D / 32)) << p.page_shift);
+    codes = base + row * (D / 2) + 4 * r.sub;
+    scale = base + ((D / 2) << p.page_shift) + row * (D / 32) + (r.sub >> 2);
 }
 
-template <class E, int D>
-__global__ __launch_bounds__(256) void cache4_write_kernel(RowParams p) {
+template <class E, int D, int U>
+__global__ __launch_bounds__(256) void cache4_write_kernel(RowParams p, unsigned int items) {
     using elem = typename E::elem;
     typedef elem vec __attribute__((ext_vector_type(8)));
-    constexpr int LPR = D / 8;
-    const long item = (long)blockIdx.x * 256 + threadIdx.x;
-    const int sub = (int)(item % LPR);
-    const long rowid = item / LPR;                          // [T][2][Hk]
-    const int per = 2 * p.Hk;
-    const long t = rowid / per;
-    if (t >= p.T) return;
-    const int which = (int)(rowid - t * per) >= p.Hk, h = (int)(rowid - t * per) - which * p.Hk;
-    const int slot = p.slots[t];
-    if (slot < 0 || (slot >> p.page_shift) >= p.n_pages) return;
-    const vec x = *(const vec*)((const elem*)p.src[which] + t * p.st[which][0] + h * p.st[which][1] + 8 * sub);
-    // magnitudes as integers: they order like the values, and infinities and NaN stay above all others
-    unsigned int top = 0;
+    const unsigned int first = blockIdx.x * (256u * U) + threadIdx.x;
+    RowItem r[U];
+    vec x[U];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint((float)x[e]) & 0x7fffffffu);
-    top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));     // over the block's four lanes
-    top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));
-    int byte = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u);                // (7 * 2^s has the fraction 0.75)
-    byte = min(max(byte, 1), 252);
-    const float scale = __uint_as_float((unsigned int)byte << 23);
-    unsigned int codes = 0;
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[0], (float)x[1], scale, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[2], (float)x[3], scale, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[4], (float)x[5], scale, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[6], (float)x[7], scale, 3);
-    if (top >= 0x7f800000u) { byte = 255; codes = 0; }
-    int row;
-    unsigned char* base = row_base<D>(p, slot, h, which, row);
-    *(unsigned int*)(base + row * (D / 2) + 4 * sub) = codes;
-    if ((sub & 3) == 0) base[((D / 2) << p.page_shift) + row * (D / 32) + (sub >> 2)] = (unsigned char)byte;
-}
-
-template <class E, int D>
-__global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p) {
-    using elem = typename E::elem;
-    typedef elem vec __attribute__((ext_vector_type(8)));
-    constexpr int LPR = D / 8;
-    const long item = (long)blockIdx.x * 256 + threadIdx.x;
-    const int sub = (int)(item % LPR);
-    const long rowid = item / LPR;
-    const int per = 2 * p.Hk;
-    const long t = rowid / per;
-    if (t >= p.T) return;
-    const int which = (int)(rowid - t * per) >= p.Hk, h = (int)(rowid - t * per) - which * p.Hk;
-    const int slot = p.slots[t];
-    if (slot < 0 || (slot >> p.page_shift) >= p.n_pages) return;
-    int row;
-    const unsigned char* base = row_base<D>(p, slot, h, which, row);
-    const unsigned int codes = *(const unsigned int*)(base + row * (D / 2) + 4 * sub);
-    const unsigned int byte = base[((D / 2) << p.page_shift) + row * (D / 32) + (sub >> 2)];
-    // 2^-127 is no normal number: byte 0, which no write leaves, is read through 2^-126 and halved
-    const float scale = byte == 255u ? __builtin_nanf("") : __uint_as_float(max(byte, 1u) << 23);
-    const float half = byte == 0u ? 0.5f : 1.f;
-    vec y;
+    for (int u = 0; u < U; ++u) r[u] = row_item<D>(p, first + 256u * u, items);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const unsigned int c = codes >> (4 * e);
-        const unsigned int m = c & 7u;
-        // level of three bits: two of exponent, one of fraction; 0.5 and 0 below
-        const float level = m < 2u ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-        y[e] = (elem)(((c & 8u) ? -level : level) * scale * half);
+    for (int u = 0; u < U; ++u)
+        x[u] = *(const vec*)((const elem*)p.src[r[u].which] + r[u].t * p.st[r[u].which][0] + r[u].h * p.st[r[u].which][1] + 8 * r[u].sub);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        // magnitudes as integers: they order like the values, and infinities and NaN stay above all others
+        unsigned int top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint((float)x[u][e]) & 0x7fffffffu);
+        top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));     // over the block's four lanes
+        top = max(top, (unsigned int)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));
+        int byte = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u);                // (7 * 2^s has the fraction 0.75)
+        byte = min(max(byte, 1), 252);
+        const float scale = __uint_as_float((unsigned int)byte << 23);
+        unsigned int codes = 0;
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[u][0], (float)x[u][1], scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[u][2], (float)x[u][3], scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[u][4], (float)x[u][5], scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, (float)x[u][6], (float)x[u][7], scale, 3);
+        if (top >= 0x7f800000u) { byte = 255; codes = 0; }
+        unsigned char *to, *to_scale;
+        row_place<D>(p, r[u], to, to_scale);
+        if (r[u].on) {
+            *(unsigned int*)to = codes;
+            if ((r[u].sub & 3) == 0) *to_scale = (unsigned char)byte;
+        }
     }
-    *(vec*)((elem*)p.dst[which] + t * p.st[which][0] + h * p.st[which][1] + 8 * sub) = y;
+}
+
+template <class E, int D, int U>
+__global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned int items) {
+    using elem = typename E::elem;
+    typedef elem vec __attribute__((ext_vector_type(8)));
+    const unsigned int first = blockIdx.x * (256u * U) + threadIdx.x;
+    RowItem r[U];
+    unsigned int codes[U], byte[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = row_item<D>(p, first + 256u * u, items);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        unsigned char *from, *from_scale;
+        row_place<D>(p, r[u], from, from_scale);
+        codes[u] = *(const unsigned int*)from;
+        byte[u] = *from_scale;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        // 2^-127 is no normal number: byte 0, which no write leaves, is read through 2^-126 and halved
+        const float scale = byte[u] == 255u ? __builtin_nanf("") : byte[u] == 0u ? 0.5f * __uint_as_float(1u << 23) : __uint_as_float(byte[u] << 23);
+        const auto v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 1);
+        const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 3);
+        const float v[8] = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+        vec y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (elem)(v[e] * scale);
+        if (r[u].on) *(vec*)((elem*)p.dst[r[u].which] + r[u].t * p.st[r[u].which][0] + r[u].h * p.st[r[u].which][1] + 8 * r[u].sub) = y;
+    }
 }
 
 }  // namespace ea
@@ -290,7 +316,22 @@ RowParams row_params(void* cache, const int32_t* slots, const int64_t* ks, const
     p.T = T; p.Hk = Hk; p.page_shift = cache_page_shift(page); p.n_pages = n_pages;
     return p;
 }
-unsigned int row_groups(int T, int Hk, int d) { return (unsigned int)(((long)T * 2 * Hk * (d / 8) + 255) / 256); }
+template <bool WRITE, class E, int D, int U> void rows_launch(const RowParams& p, unsigned int items, hipStream_t s) {
+    const dim3 grid((unsigned int)(((long)items + 256 * U - 1) / (256 * U)));
+    if constexpr (WRITE) hipLaunchKernelGGL((cache4_write_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
+    else hipLaunchKernelGGL((cache4_read_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
+}
+template <bool WRITE> int rows_run(const RowParams& p, int d, int dtype, hipStream_t s) {
+    const unsigned int items = (unsigned int)((long)p.T * 2 * p.Hk * (d / 8));
+    const bool many = items >= ROWS_MANY;
+    auto pick = [&](auto e) {
+        using E = decltype(e);
+        if (d == 64) { if (many) rows_launch<WRITE, E, 64, 4>(p, items, s); else rows_launch<WRITE, E, 64, 1>(p, items, s); }
+        else { if (many) rows_launch<WRITE, E, 128, 4>(p, items, s); else rows_launch<WRITE, E, 128, 1>(p, items, s); }
+    };
+    if (dtype == EA_BF16) pick(Bf16{}); else pick(F32{});
+    return cache_launched();
+}
 
 }  // namespace
 
@@ -325,11 +366,7 @@ int entmax_attn_cache4_write(const void* K, const void* V, const int64_t* k_stri
     if (T == 0) return EA_OK;
     RowParams p = row_params(cache, slots, k_strides, v_strides, T, Hk, page_size, n_pages);
     p.src[0] = K; p.src[1] = V;
-    const dim3 grid(row_groups(T, Hk, d));
-    hipStream_t s = (hipStream_t)hip_stream;
-    if (dtype == EA_BF16) { if (d == 64) hipLaunchKernelGGL((cache4_write_kernel<Bf16, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_write_kernel<Bf16, 128>), grid, dim3(256), 0, s, p); }
-    else { if (d == 64) hipLaunchKernelGGL((cache4_write_kernel<F32, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_write_kernel<F32, 128>), grid, dim3(256), 0, s, p); }
-    return cache_launched();
+    return rows_run<true>(p, d, dtype, (hipStream_t)hip_stream);
 }
 
 int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
@@ -339,11 +376,7 @@ int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, vo
     if (T == 0) return EA_OK;
     RowParams p = row_params(const_cast<void*>(cache), slots, k_strides, v_strides, T, Hk, page_size, n_pages);
     p.dst[0] = K; p.dst[1] = V;
-    const dim3 grid(row_groups(T, Hk, d));
-    hipStream_t s = (hipStream_t)hip_stream;
-    if (dtype == EA_BF16) { if (d == 64) hipLaunchKernelGGL((cache4_read_kernel<Bf16, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_read_kernel<Bf16, 128>), grid, dim3(256), 0, s, p); }
-    else { if (d == 64) hipLaunchKernelGGL((cache4_read_kernel<F32, 64>), grid, dim3(256), 0, s, p); else hipLaunchKernelGGL((cache4_read_kernel<F32, 128>), grid, dim3(256), 0, s, p); }
-    return cache_launched();
+    return rows_run<false>(p, d, dtype, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

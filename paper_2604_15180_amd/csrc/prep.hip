@@ -89,57 +89,76 @@ EA_DEV void angles(const PrepParams& p, int token, int sub, float (&c)[4], float
     }
 }
 
+// Several heads' rows are on their way at once (the compiler does not unroll a loop with cross-lane sums by itself, and one row
+// at a time does not cover the memory's latency: 32768 tokens of 32 heads, D = 128, bf16, 123 -> 115 us; two rows 118, eight 114; 111 with
+// the first ones asked for before the angles: 4.8 TB/s of reads and writes).
 template <class E, int D, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void qk_prep_kernel(PrepParams p) {
     using elem = typename E::elem;
-    constexpr int LPR = D / 8, TPG = 256 / LPR;
+    constexpr int LPR = D / 8, TPG = 256 / LPR, HB = 4;
     const int sub = threadIdx.x % LPR;
     const int token = blockIdx.x * TPG + threadIdx.x / LPR;
     if (token >= p.tokens) return;                       // (no exchange crosses the lanes of a row)
     const int b = token / p.N, n = token - b * p.N;
-    float c[4], s[4];
-    angles(p, token, sub, c, s);
     int pa, pb;
     pair_place<D, NEIGHBOURS>(sub, p.pairs, pa, pb);
-    const int h_all = p.H[0] + p.H[1];
-    const int h0 = blockIdx.y * p.heads_per_group, h1 = min(h_all, h0 + p.heads_per_group);
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
+    const int h0 = blockIdx.y * p.heads_per_group, h1 = min(p.H[0] + p.H[1], h0 + p.heads_per_group);
+    auto row = [&](int which, int h) { return (const elem*)p.x[which] + b * p.st[which][0] + n * p.st[which][1] + h * p.st[which][2]; };
+    // heads first .. last - 1 of q (which = 0) or k are this work-group's
+    auto heads_of = [&](int which, int& first, int& last) {
         const int base = which ? p.H[0] : 0;
-        const int first = max(h0, base) - base, last = min(h1, base + p.H[which]) - base;
+        first = max(h0, base) - base;
+        last = min(h1, base + p.H[which]) - base;
+    };
+    Pairs v[HB];
+    auto load = [&](int which, int h, int last) {
+#pragma unroll
+        for (int k = 0; k < HB; ++k) v[k] = load_pairs<NEIGHBOURS>(row(which, min(h + k, last - 1)), pa, pb);
+    };
+    int first, last;
+    const int start = h0 < p.H[0] ? 0 : 1;
+    heads_of(start, first, last);
+    load(start, first, last);                            // (on their way while the angles are formed)
+    float c[4], s[4];
+    angles(p, token, sub, c, s);
+#pragma unroll 1
+    for (int which = start; which < 2; ++which) {
+        heads_of(which, first, last);
         if (first >= last) continue;
         Pairs w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.a[e] = w.b[e] = 1.f;
         if (p.w[which]) w = load_pairs<NEIGHBOURS>(p.w[which], pa, pb);
-        const elem* x = (const elem*)p.x[which] + b * p.st[which][0] + n * p.st[which][1];
         elem* y = (elem*)p.y[which] + ((long)b * p.H[which] * p.N + n) * D;
-#pragma unroll 4
-        for (int h = first; h < last; ++h) {
-            Pairs v = load_pairs<NEIGHBOURS>(x + h * p.st[which][2], pa, pb);
-            float rstd = 1.f;
-            if (p.norm) {
-                float sq = 0.f;
+        for (int h = first; h < last; h += HB) {
+            if (which != start || h != first) load(which, h, last);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sq = fmaf(v.a[e], v.a[e], fmaf(v.b[e], v.b[e], sq));
-                rstd = rsqrtf(group_sum<LPR>(sq) * (1.f / D) + p.eps);
-            }
+            for (int k = 0; k < HB; ++k) {
+                float rstd = 1.f;
+                if (p.norm) {
+                    float sq = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = v.a[e] * rstd * w.a[e], bb = v.b[e] * rstd * w.b[e];
-                v.a[e] = a * c[e] - bb * s[e];
-                v.b[e] = a * s[e] + bb * c[e];
+                    for (int e = 0; e < 4; ++e) sq = fmaf(v[k].a[e], v[k].a[e], fmaf(v[k].b[e], v[k].b[e], sq));
+                    rstd = rsqrtf(group_sum<LPR>(sq) * (1.f / D) + p.eps);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = v[k].a[e] * rstd * w.a[e], bb = v[k].b[e] * rstd * w.b[e];
+                    v[k].a[e] = a * c[e] - bb * s[e];
+                    v[k].b[e] = a * s[e] + bb * c[e];
+                }
+                if (h + k < last) store_pairs<NEIGHBOURS>(y + (long)(h + k) * p.N * D, pa, pb, v[k]);
             }
-            store_pairs<NEIGHBOURS>(y + (long)h * p.N * D, pa, pb, v);
         }
     }
 }
 
-// A work-group takes every gridDim.x-th set of tokens and leaves one row of sums of dw; qk_prep_dw_kernel adds the rows.
+// A work-group takes every gridDim.x-th set of tokens and a part of the heads, and leaves one row of sums of dw; qk_prep_dw_kernel adds
+// the rows.  (16384 tokens of 32 heads, D = 64, bf16: 44 us, 6.1 TB/s; with one row at a time on its way 52.)
 template <class E, int D, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void qk_prep_bwd_kernel(PrepParams p) {
     using elem = typename E::elem;
-    constexpr int LPR = D / 8, TPG = 256 / LPR;
+    constexpr int LPR = D / 8, TPG = 256 / LPR, HB = 2;
     __shared__ float sums[4][2][D];
     const int sub = threadIdx.x % LPR;
     int pa, pb;
@@ -149,10 +168,24 @@ __global__ __launch_bounds__(256) void qk_prep_bwd_kernel(PrepParams p) {
     for (int which = 0; which < 2; ++which)
 #pragma unroll
         for (int e = 0; e < 4; ++e) dw[which].a[e] = dw[which].b[e] = 0.f;
+    const int p0 = blockIdx.y * p.heads_per_group, p1 = min(p.H[0] + p.H[1], p0 + p.heads_per_group);
     for (long set = blockIdx.x; set * TPG < p.tokens; set += gridDim.x) {
         const int token = (int)(set * TPG) + threadIdx.x / LPR;
         if (token >= p.tokens) break;
         const int b = token / p.N, n = token - b * p.N;
+        Pairs gr[HB], v[HB];
+        auto load = [&](int which, int h0, int last) {
+            const elem* x = (const elem*)p.x[which] + b * p.st[which][0] + n * p.st[which][1];
+            const float* dy = p.dy[which] + ((long)b * p.H[which] * p.N + n) * D;
+#pragma unroll
+            for (int k = 0; k < HB; ++k) {
+                const int h = min(h0 + k, last - 1);
+                gr[k] = load_pairs<NEIGHBOURS>(dy + (long)h * p.N * D, pa, pb);
+                v[k] = load_pairs<NEIGHBOURS>(x + h * p.st[which][2], pa, pb);
+            }
+        };
+        const int start = p0 < p.H[0] ? 0 : 1;
+        load(start, start ? p0 - p.H[0] : p0, start ? p1 - p.H[0] : min(p1, p.H[0]));        // (on their way while the angles are formed)
         float c[4], s[4];
         angles(p, token, sub, c, s);
 #pragma unroll
@@ -161,42 +194,45 @@ __global__ __launch_bounds__(256) void qk_prep_bwd_kernel(PrepParams p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) w.a[e] = w.b[e] = 1.f;
             if (p.w[which]) w = load_pairs<NEIGHBOURS>(p.w[which], pa, pb);
-            const elem* x = (const elem*)p.x[which] + b * p.st[which][0] + n * p.st[which][1];
             elem* dx = (elem*)p.y[which] + b * p.dst[which][0] + n * p.dst[which][1];
-            const float* dy = p.dy[which] + ((long)b * p.H[which] * p.N + n) * D;
-#pragma unroll 2
-            for (int h = 0; h < p.H[which]; ++h) {
-                Pairs g = load_pairs<NEIGHBOURS>(dy + (long)h * p.N * D, pa, pb);
-                const Pairs v = load_pairs<NEIGHBOURS>(x + h * p.st[which][2], pa, pb);
+            const int base = which ? p.H[0] : 0;
+            const int first = max(p0, base) - base, last = min(p1, base + p.H[which]) - base;
+            for (int h0 = first; h0 < last; h0 += HB) {
+                if (which != start || h0 != first) load(which, h0, last);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float ga = g.a[e] * c[e] + g.b[e] * s[e];
-                    g.b[e] = g.b[e] * c[e] - g.a[e] * s[e];
-                    g.a[e] = ga;
-                }
-                if (p.norm) {
-                    float sq = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sq = fmaf(v.a[e], v.a[e], fmaf(v.b[e], v.b[e], sq));
-                    const float rstd = rsqrtf(group_sum<LPR>(sq) * (1.f / D) + p.eps);
-                    float dot = 0.f;
-                    Pairs xh;
+                for (int k = 0; k < HB; ++k) {
+                    if (h0 + k >= last) break;
+                    Pairs& g = gr[k];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        xh.a[e] = v.a[e] * rstd; xh.b[e] = v.b[e] * rstd;
-                        dw[which].a[e] = fmaf(g.a[e], xh.a[e], dw[which].a[e]);
-                        dw[which].b[e] = fmaf(g.b[e], xh.b[e], dw[which].b[e]);
-                        g.a[e] *= w.a[e]; g.b[e] *= w.b[e];
-                        dot = fmaf(g.a[e], xh.a[e], fmaf(g.b[e], xh.b[e], dot));
+                        const float ga = g.a[e] * c[e] + g.b[e] * s[e];
+                        g.b[e] = g.b[e] * c[e] - g.a[e] * s[e];
+                        g.a[e] = ga;
                     }
-                    dot = group_sum<LPR>(dot) * (1.f / D);
+                    if (p.norm) {
+                        float sq = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        g.a[e] = rstd * (g.a[e] - xh.a[e] * dot);
-                        g.b[e] = rstd * (g.b[e] - xh.b[e] * dot);
+                        for (int e = 0; e < 4; ++e) sq = fmaf(v[k].a[e], v[k].a[e], fmaf(v[k].b[e], v[k].b[e], sq));
+                        const float rstd = rsqrtf(group_sum<LPR>(sq) * (1.f / D) + p.eps);
+                        float dot = 0.f;
+                        Pairs xh;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            xh.a[e] = v[k].a[e] * rstd; xh.b[e] = v[k].b[e] * rstd;
+                            dw[which].a[e] = fmaf(g.a[e], xh.a[e], dw[which].a[e]);
+                            dw[which].b[e] = fmaf(g.b[e], xh.b[e], dw[which].b[e]);
+                            g.a[e] *= w.a[e]; g.b[e] *= w.b[e];
+                            dot = fmaf(g.a[e], xh.a[e], fmaf(g.b[e], xh.b[e], dot));
+                        }
+                        dot = group_sum<LPR>(dot) * (1.f / D);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            g.a[e] = rstd * (g.a[e] - xh.a[e] * dot);
+                            g.b[e] = rstd * (g.b[e] - xh.b[e] * dot);
+                        }
                     }
+                    store_pairs<NEIGHBOURS>(dx + (h0 + k) * p.dst[which][2], pa, pb, g);
                 }
-                store_pairs<NEIGHBOURS>(dx + h * p.dst[which][2], pa, pb, g);
             }
         }
     }
@@ -216,19 +252,29 @@ __global__ __launch_bounds__(256) void qk_prep_bwd_kernel(PrepParams p) {
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * D; i += 256) {
         const float* s0 = &sums[0][0][0] + i;
-        p.part[(long)blockIdx.x * 2 * D + i] = (s0[0] + s0[2 * D]) + (s0[4 * D] + s0[6 * D]);
+        p.part[((long)blockIdx.y * gridDim.x + blockIdx.x) * 2 * D + i] = (s0[0] + s0[2 * D]) + (s0[4 * D] + s0[6 * D]);
     }
 }
 
-// dw[which][i] = sum over the rows of `part`, in 64 bits: 64 columns per work-group, sixteen threads to a column
+// dw[which][i] = sum over the rows of `part`, in 64 bits: sixteen columns per work-group, 64 threads to a column (with 64 columns and
+// sixteen threads a launch took 10 us for 1024 rows: each thread's 64 loads stood in a row)
 __global__ __launch_bounds__(1024) void qk_prep_dw_kernel(const float* part, float* dwq, float* dwk, int rows, int D) {
-    __shared__ double sums[16][64];
-    const int col = threadIdx.x & 63, slice = threadIdx.x >> 6, i = blockIdx.x * 64 + col;
+    constexpr int COLS = 16, U = 4;
+    __shared__ double sums[16][COLS];
+    const int col = threadIdx.x % COLS, slice = threadIdx.x / COLS, i = blockIdx.x * COLS + col;
     double a = 0.0;
-    for (int r = slice; r < rows; r += 16) a += (double)part[(long)r * 2 * D + i];
-    sums[slice][col] = a;
+    for (int r0 = slice; r0 < rows; r0 += 64 * U) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = r0 + 64 * u < rows ? part[(long)(r0 + 64 * u) * 2 * D + i] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) a += (double)v[u];
+    }
+    a += __shfl_xor(a, 16);                 // a wave holds four slices of the sixteen columns
+    a += __shfl_xor(a, 32);
+    if ((threadIdx.x & 63) < COLS) sums[threadIdx.x >> 6][col] = a;
     __syncthreads();
-    if (slice == 0) {
+    if (threadIdx.x < COLS) {
 #pragma unroll
         for (int k = 1; k < 16; ++k) a += sums[k][col];
         float* out = i < D ? dwq : dwk;
@@ -309,6 +355,17 @@ void prep_params(PrepParams& p, const void* q, const void* k, const float* wq, c
     p.eps = eps; p.norm = norm;
 }
 
+// Work-groups: one for `sets` of tokens, and where these are fewer than `enough` one for each part of the heads as well.  (The angles of
+// a token are formed once for each part.  Gradient of 16384 tokens of 32 heads: 512 work-groups 44 us, 1024 of half the heads 52; of
+// 2174 tokens of 10 heads: 136 work-groups 11.0, 544 10.0.)
+dim3 prep_grid(PrepParams& p, int sets, int enough) {
+    const int heads = p.H[0] + p.H[1];
+    int parts = 1;
+    while (parts < heads && (long)sets * parts < enough) parts *= 2;
+    p.heads_per_group = (heads + parts - 1) / parts;
+    return dim3(sets, (heads + p.heads_per_group - 1) / p.heads_per_group);
+}
+
 int prep_launched() {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
@@ -342,11 +399,7 @@ int entmax_attn_qk_norm_rope_fwd(const void* q, const void* k, void* q_out, void
     PrepParams p{};
     prep_params(p, q, k, q_weight, k_weight, positions, inv_freq, B, Hq, Hk, N, rot, n_axes, sections, norm, eps, q_strides, k_strides);
     p.y[0] = q_out; p.y[1] = k_out;
-    const int gx = (p.tokens + tokens_per_group(d) - 1) / tokens_per_group(d), heads = Hq + Hk;
-    int parts = 1;
-    while (parts < heads && (long)gx * parts < 1024) parts *= 2;
-    p.heads_per_group = (heads + parts - 1) / parts;
-    const dim3 grid(gx, (heads + p.heads_per_group - 1) / p.heads_per_group);
+    const dim3 grid = prep_grid(p, (p.tokens + tokens_per_group(d) - 1) / tokens_per_group(d), 1024);
     hipStream_t s = (hipStream_t)hip_stream;
     if (dtype == EA_BF16) { if (d == 64) fwd_launch<Bf16, 64>(p, interleaved, grid, s); else fwd_launch<Bf16, 128>(p, interleaved, grid, s); }
     else { if (d == 64) fwd_launch<F32, 64>(p, interleaved, grid, s); else fwd_launch<F32, 128>(p, interleaved, grid, s); }
@@ -382,13 +435,14 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
     for (int i = 0; i < 3; ++i) { p.dst[0][i] = dq_strides[i]; p.dst[1][i] = dk_strides[i]; }
     p.part = want_dw ? (float*)workspace : nullptr;
     const int sets = (p.tokens + tokens_per_group(d) - 1) / tokens_per_group(d);
-    const int groups = sets < BWD_GROUPS ? sets : BWD_GROUPS;
+    dim3 grid = prep_grid(p, sets, 512);
+    if (grid.x * grid.y > BWD_GROUPS) grid.x = BWD_GROUPS / grid.y;
+    const int groups = grid.x * grid.y;
     hipStream_t s = (hipStream_t)hip_stream;
-    const dim3 grid(groups);
     if (dtype == EA_BF16) { if (d == 64) bwd_launch<Bf16, 64>(p, interleaved, grid, s); else bwd_launch<Bf16, 128>(p, interleaved, grid, s); }
     else { if (d == 64) bwd_launch<F32, 64>(p, interleaved, grid, s); else bwd_launch<F32, 128>(p, interleaved, grid, s); }
     if (want_dw)
-        hipLaunchKernelGGL(qk_prep_dw_kernel, dim3(2 * d / 64), dim3(1024), 0, s, p.part, dq_weight, dk_weight, groups, d);
+        hipLaunchKernelGGL(qk_prep_dw_kernel, dim3(2 * d / 16), dim3(1024), 0, s, p.part, dq_weight, dk_weight, groups, d);
     return prep_launched();
 }
 
