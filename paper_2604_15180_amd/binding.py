@@ -431,7 +431,7 @@ def entmax_attn_cache_tables(lens, new_lens, block_table, free_pages, free_count
     if out is None:
         if max_tokens < 0:
             raise ValueError(f"{call}: max_tokens must not be negative")
-        out = torch.empty(2 * R + 5 + 2 * max_tokens, dtype=torch.int32, device=lens.device).split([R, R + 1, max_tokens, max_tokens, 4])
+        out = torch.empty(2 * R + 5 + 2 * max_tokens, dtype=torch.int32, device=lens.device).split_with_sizes([R, R + 1, max_tokens, max_tokens, 4])
     else:
         for name, t, shape in zip(("lens_out", "token_start", "slots", "positions", "status"), out, shapes):
             _int32(call, name, t, shape)

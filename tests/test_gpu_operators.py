@@ -389,6 +389,7 @@ DECODE = [
     ([6000, 100], 4, 2, 64, "bf16", 64, 1.5, 0.2),             # flat: more candidates than the second kernel's buffer
     ([5000], 2, 2, 128, "f32", 32, 1.1, 1.0),                  # r = 10: hundreds of keys in the support
     ([3000], 2, 1, 64, "bf16", 16, 1.02, 1.5),                 # r = 50
+    ([2000], 2, 1, 128, "f32", 16, 1.004, 1.5),                # r = 250
     ([70000], 8, 2, 64, "bf16", 128, 1.5, 1.5),
 ]
 
