@@ -145,19 +145,25 @@ EA_DEV unsigned int c4_ordered(float f) {
 EA_DEV float c4_from_ordered(unsigned int u) { return __uint_as_float((u & 0x80000000u) ? (u ^ 0x80000000u) : ~u); }
 
 // Tiles: at D = 128 sixteen keys, one instruction per term; at D = 64 two sets of sixteen keys, the lower half of the lanes
-// (contraction indices 0 .. 63 of the operand) one, the upper half the other; the query terms stand in both halves of their operand,
-// and the keys are worked on one set at a time, with zeros in place of the other's.  Result: lane (n, g) holds head n's scores with keys
-// 4 g .. 4 g + 3 of a set.  A wave keeps two blocks of 64 keys on their way: as soon as the matrix cores have taken a tile, the same
-// tile of the block after the next is requested.  The addresses of all its keys are formed at once, a lane for each sixteen.
-template <class E, int D>
+// (contraction indices 0 .. 63 of the operand) one, the upper half the other.  Then (PAIR) up to eight query heads stand in columns 0 .. 7
+// with their terms in the lower indices, for the first set, and once more in columns 8 .. 15 in the upper ones, for the second,
+// with zeros elsewhere: both sets in one instruction per term.  More heads have their terms in both halves, and the keys are worked on
+// one set at a time, with zeros in place of the other's (32 heads x 131072 keys, one head a key head: 34 us, PAIR 30; fp32 queries 41 and 32).
+// Result: lane (n, g) holds column n's scores with keys 4 g .. 4 g + 3 of a set.  A wave keeps two blocks of 64 keys on their way: as soon as
+// the matrix cores have taken a tile, the same tile of the block after the next is requested.  The addresses of all its keys are
+// formed at once, a lane for each sixteen.
+template <class E, int D, bool PAIR>
 __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Params p) {
     constexpr int NT = sizeof(typename E::elem) == 2 ? 3 : 5, SETS = 128 / D, TK = 16 * SETS, U = C4_BLOCK / TK;
+    constexpr int PASSES = PAIR ? 1 : SETS, COLS = PAIR ? 8 : 16;         // instructions of a tile and term; query heads side by side
+    static_assert(!PAIR || SETS == 2, "two sets to a tile");
     constexpr int ROW = D / 2, SROW = D / 32;
     __shared__ unsigned int smax[16];                       // ordered bits of the work-group's running maxima
     __shared__ int words[NT][8][64];
     __shared__ float tops[C4_WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 15, g = lane >> 4;
+    const int n = lane & 15, g = lane >> 4, col = n % COLS;
+    const int set0 = PAIR ? n / COLS : 0;                   // the set the lane's column is for
     // Short requests have few parts, and the work-groups that find nothing to do must not fall on some of the XCDs, or some of the 32
     // CUs of each, to which consecutive work-groups are dealt in turn.  So the part is the slowest index (as the fastest one 48
     // requests of 64 .. 32768 tokens took 98 us in place of 50: all their first parts stood on one XCD), and the requests move
@@ -168,8 +174,8 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
     // the waves take the work-group's blocks in turn, so that a request shorter than its part of the keys is all four waves' work
     const int c0 = chunk * C4_WAVES * p.part;
     auto block_key = [&](int i) { return c0 + (i * C4_WAVES + wave) * C4_BLOCK; };        // first key of the wave's block i
-    const bool live = cg * 16 + n < p.G;
-    const long head = (long)req * p.Hq + kvh * p.G + (live ? cg * 16 + n : 0);
+    const bool live = cg * 16 + col < p.G;
+    const long head = (long)req * p.Hq + kvh * p.G + (live ? cg * 16 + col : 0);
     // length, pages and query are asked for together, and the first keys before the query is worked on.  Lane 4 i + j: the sixteen
     // keys j of block i (C4_MAX_PART: at most eight blocks).
     const int len = p.lens[req];
@@ -214,7 +220,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
     auto compute = [&](auto more, Batch& x, int i) {
         const int t0 = block_key(i);
         const bool part_of = t0 + C4_BLOCK > k1;
-        f32x4 s[U][SETS];
+        f32x4 s[U][PASSES];
         float best = -INFINITY;
         int top = 0;
 #pragma unroll
@@ -223,10 +229,10 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
             if (part_of && t0 + u * TK + (SETS == 2 ? 16 * (g >> 1) : 0) + n >= k1) { x.a[u] = i32x4{0, 0, 0, 0}; x.sc[u] = 1; }
             top = max(top, x.sc[u]);
 #pragma unroll
-            for (int set = 0; set < SETS; ++set) {
+            for (int set = 0; set < PASSES; ++set) {
                 i32x8 av = {x.a[u][0], x.a[u][1], x.a[u][2], x.a[u][3], 0, 0, 0, 0};
                 int sc = x.sc[u];
-                if (SETS == 2 && (g >> 1) != set) { av = i32x8{0, 0, 0, 0, 0, 0, 0, 0}; sc = 1; }
+                if (PASSES == 2 && (g >> 1) != set) { av = i32x8{0, 0, 0, 0, 0, 0, 0, 0}; sc = 1; }
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = NT - 1; t >= 0; --t)
@@ -238,28 +244,29 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int set = 0; set < SETS; ++set)
+            for (int set = 0; set < PASSES; ++set)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    if (part_of && t0 + u * TK + 16 * set + 4 * g + k >= k1) s[u][set][k] = -INFINITY;
+                    if (part_of && t0 + u * TK + 16 * (set0 + set) + 4 * g + k >= k1) s[u][set][k] = -INFINITY;
                     best = fmaxf(best, s[u][set][k]);
                 }
+        if constexpr (PAIR) best = fmaxf(best, dpp_move<0x128>(best));          // (row_ror 8: the head's other column)
         best = across16_max(best);
         if (__any(top >= limit) || bad || odd) best = INFINITY;
         if (!live) best = -INFINITY;
-        const float shared_max = c4_from_ordered(__hip_atomic_load(&smax[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+        const float shared_max = c4_from_ordered(__hip_atomic_load(&smax[col], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         lmax = fmaxf(lmax, best);
         const float m = fmaxf(lmax, shared_max);
         if (live && g == 0) bmax[t0 / C4_BLOCK] = best;
         // (a maximum that is infinite: NaN, nothing is kept, nor is anything needed)
         const bool keep = best >= m - p.win - 1e-6f * fabsf(m) && live;
         if (!__any(keep)) return;
-        if (g == 0 && best > shared_max) atomicMax(&smax[n], c4_ordered(best));
+        if (g == 0 && best > shared_max) atomicMax(&smax[col], c4_ordered(best));
         if (keep) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int set = 0; set < SETS; ++set) *(f32x4*)(scores + t0 + u * TK + 16 * set + 4 * g) = s[u][set];
+                for (int set = 0; set < PASSES; ++set) *(f32x4*)(scores + t0 + u * TK + 16 * (set0 + set) + 4 * g) = s[u][set];
         }
     };
     constexpr auto more = std::true_type{};
@@ -270,6 +277,12 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 #pragma unroll
     for (int u = 0; u < U; ++u) if (mine > 1) load(x1, 1, u);
     limit = query_terms<E, D, NT>(qrow, wave, words, tops, q, odd);
+    if constexpr (PAIR) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) { if (set0) q.t[t][w] = 0; else q.t[t][4 + w] = 0; }
+    }
     int i = 0;
     for (; i + 3 < mine; i += 2) { compute(more, x0, i); compute(more, x1, i + 1); }
     if (i + 2 < mine) { compute(more, x0, i); compute(no_more, x1, i + 1); compute(no_more, x0, i + 2); }
@@ -316,8 +329,8 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         return;
     }
     // f(x, key) for the scores of the wave's blocks that reach into the window, in the order of their keys, a block at a time, four
-    // such loads in flight.  (The score kernel has written these blocks: its window was this one or a lower one.)
-    auto walk = [&](auto f) {
+    // such loads in flight, and then after().  (The score kernel has written these blocks: its window was this one or a lower one.)
+    auto walk = [&](auto f, auto after) {
         for (int c0 = b0; c0 < b1; c0 += 64) {
             unsigned long long todo = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
             while (todo) {
@@ -334,6 +347,26 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (key[u] >= 0) f(p.c * (s[u] - gm), key[u] + lane);       // (keys past the end were written as -inf)
+                after();
+            }
+        }
+    };
+    // The same for sums alone: g(x) for all of them, 256 keys a load.
+    auto stream = [&](auto g) {
+        for (int c0 = b0; c0 < b1; c0 += 64) {
+            const unsigned long long in = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
+#pragma unroll 1
+            for (int j = 0; j < 16; j += U) {
+                f32x4 v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    v[u] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    if (in >> (4 * (j + u) + (lane >> 4)) & 1) v[u] = *(const f32x4*)(scores + (c0 + 4 * (j + u)) * C4_BLOCK + 4 * lane);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) g(p.c * (v[u][e] - gm));
             }
         }
     };
@@ -345,7 +378,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         const int at = total + __popcll(in & ((1ull << lane) - 1ull));
         if (x >= -1.f && at < SEG) { lx[wave][at] = x; lj[wave][at] = j; }
         total += __popcll(in);
-    });
+    }, [] {});
     const bool over = total > SEG;          // then every evaluation of this wave streams its blocks instead
     // F = sum [x - tau]^r and G = sum [x - tau]^(r - 1) over the work-group, the same in every thread
     int turn = 0;
@@ -356,7 +389,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
             if (y > 0.f) { const float y1 = pow_r1<AM>(y, r); gs += y1; f = fmaf(y1, y, f); }
         };
         if (!over) for (int i = lane; i < total; i += 64) term(lx[wave][i]);
-        else walk([&](float x, int) { term(x); });
+        else stream(term);
         f = whole_wave_sum(f);
         gs = whole_wave_sum(gs);
         turn ^= 1;                          // (two sets: a wave that is ahead writes the other one)
@@ -416,11 +449,12 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         at += __popcll(in);
     };
     auto add_rows = [&](int count) {
-        for (int i0 = 0; i0 < count; i0 += U * AT_ONCE) {
-            unsigned int codes[U];
-            float ps[U];
+        constexpr int S = 4;
+        for (int i0 = 0; i0 < count; i0 += S * AT_ONCE) {
+            unsigned int codes[S];
+            float ps[S];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < S; ++u) {
                 const int i = i0 + u * AT_ONCE + rsel;
                 codes[u] = 0u; ps[u] = 0.f;
                 if (i < count) {
@@ -433,7 +467,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
                 }
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < S; ++u) {
                 const auto v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 1);
                 const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 3);
                 const float v[8] = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
@@ -443,20 +477,17 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         }
         nsup += count;
     };
+    int kept = 0;
     if (!over) {
-        int at = 0;
         for (int i0 = 0; i0 < total; i0 += 64) {
             const bool in = i0 + lane < total;
-            keep_support(in ? lx[wave][i0 + lane] : -2.f, in ? lj[wave][i0 + lane] : 0, at);
+            keep_support(in ? lx[wave][i0 + lane] : -2.f, in ? lj[wave][i0 + lane] : 0, kept);
         }
-        add_rows(at);
     } else {
-        walk([&](float x, int j) {
-            int at = 0;
-            keep_support(x, j, at);
-            add_rows(at);
-        });
+        walk([&](float x, int j) { keep_support(x, j, kept); },
+             [&] { if (kept > SEG - 64 * U) { add_rows(kept); kept = 0; } });
     }
+    add_rows(kept);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         if constexpr (LPR == 8) acc[k] += dpp_move<0x128>(acc[k]);              // (row_ror 8)
@@ -493,7 +524,9 @@ template <int D, int NW> void cache4_entmax(const Cache4Params& p, hipStream_t s
 template <class E, int D>
 void cache4_run(const Cache4Params& p, hipStream_t s) {
     const int per_group = C4_WAVES * p.part;
-    hipLaunchKernelGGL((cache4_scores_kernel<E, D>), dim3(p.Hk * p.colgroups, p.R, (p.max_len + per_group - 1) / per_group), dim3(64 * C4_WAVES), 0, s, p);
+    const dim3 grid(p.Hk * p.colgroups, p.R, (p.max_len + per_group - 1) / per_group), block(64 * C4_WAVES);
+    if (D == 64 && p.G <= 8) hipLaunchKernelGGL((cache4_scores_kernel<E, D, D == 64>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((cache4_scores_kernel<E, D, false>), grid, block, 0, s, p);
     if ((long)p.R * p.Hq < 512) cache4_entmax<D, 8>(p, s); else cache4_entmax<D, 4>(p, s);
 }
 
