@@ -379,7 +379,7 @@ def entmax_attn_qk_norm_rope_fwd(q, k, positions, inv_freq, q_weight=None, k_wei
     q_out, k_out = q.new_empty((B, Hq, N, d)), q.new_empty((B, Hk, N, d))
     _launch(dev, lib().entmax_attn_qk_norm_rope_fwd, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _row_strides(q),
             _row_strides(k), _at(q_weight), _at(k_weight), _at(positions), _at(inv_freq), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes,
-            sec, bool(interleaved), bool(norm), eps)
+            sec, bool(interleaved), bool(norm), float(eps))
     return q_out, k_out
 
 
@@ -411,7 +411,7 @@ def entmax_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_we
     _launch(dev, lib().entmax_attn_qk_norm_rope_bwd, q.data_ptr(), k.data_ptr(), dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(),
             dk.data_ptr(), _row_strides(q), _row_strides(k), _row_strides(dq), _row_strides(dk), _at(q_weight), _at(k_weight),
             _at(positions), _at(inv_freq), _at(dwq), _at(dwk), B, Hq, Hk, N, d, _dtype_code(q.dtype), rot, axes, sec, bool(interleaved),
-            bool(norm), eps, _at(ws), 0 if ws is None else ws.numel() * ws.element_size())
+            bool(norm), float(eps), _at(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return dq, dk, dwq, dwk
 
 
@@ -517,7 +517,7 @@ def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max
     O, tau, support = q.new_empty((R, Hq, d), dtype=torch.float32), q.new_empty((R, Hq), dtype=torch.float32), lens.new_empty((R, Hq))
     ws = workspace if workspace is not None else _workspace(entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len), q.device)
     _launch(dev, lib().entmax_attn_decode_cache4, q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), lens.data_ptr(), O.data_ptr(),
-            tau.data_ptr(), support.data_ptr(), R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, alpha,
+            tau.data_ptr(), support.data_ptr(), R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, float(alpha),
             ws.data_ptr(), ws.numel() * ws.element_size())
     return O, tau, support
 

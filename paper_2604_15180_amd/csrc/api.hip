@@ -482,7 +482,7 @@ const char* entmax_attn_strerror(int code) {
         case EA_OK: return "ok";
         case EA_ERR_NULL: return "a required pointer is NULL";
         case EA_ERR_ALPHA: return "alpha must be finite and in (1, 3]";
-        case EA_ERR_SHAPE: return "bad shape: need B,H > 0, N a positive multiple of 64 (<= 131072), d in {64, 128}";
+        case EA_ERR_SHAPE: return "bad shape: need B,H > 0, N a positive multiple of 64 (<= 131072), d in {64, 128}, or the limits the call's own description gives";
         case EA_ERR_DTYPE: return "unknown dtype";
         case EA_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned, or too small";
         case EA_ERR_HIP: return "a HIP call failed (see entmax_attn_last_hip_error)";

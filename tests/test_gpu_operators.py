@@ -632,3 +632,46 @@ def test_chunked_prefill_attends_to_the_cache_as_it_is(ea):
     O, tau, _ = ea.entmax_attn_fwd(q, K, V, 1.5, True)
     o, t, _ = ea.entmax_attn_decode_cache4(q[:, :, -1].contiguous(), cache, i32([[0, 1, 2]]), i32([N]), 1.5, page)
     assert (O[:, :, -1] - o).abs().max() <= 1e-2 and (tau[:, :, -1] - t).abs().max() <= 1e-3      # the forward's bars for bf16
+
+
+# ---- past 2^32 bytes ----------------------------------------------------------------------------------------------
+
+def test_cache_beyond_four_gigabytes(ea):
+    # pages at the end of a cache of 5.6 GB
+    Hk, d, page, n, pages = 8, 128, 256, 600, 20000
+    cache = ea.entmax_attn_cache4_empty(pages, Hk, d, page)
+    assert cache.numel() > 2 ** 32
+    ids = [pages - 1, pages // 2, pages - 7]
+    g = torch.Generator().manual_seed(50)
+    k, v = torch.randn(n, Hk, d, generator=g), torch.randn(n, Hk, d, generator=g)
+    pos = torch.arange(n)
+    slots = (torch.tensor(ids)[pos // page] * page + pos % page).to(torch.int32).cuda()
+    ea.entmax_attn_cache4_write(k.cuda(), v.cuda(), slots, cache, page)
+    K, V = ea.entmax_attn_cache4_read(cache, slots, page, d, torch.float32)
+    ks, vs = ref.quantise(k.double().numpy())[2], ref.quantise(v.double().numpy())[2]
+    np.testing.assert_array_equal(K.double().cpu().numpy(), ks)
+    np.testing.assert_array_equal(V.double().cpu().numpy(), vs)
+    q = torch.randn(1, 16, d, generator=g).to(torch.bfloat16)
+    got = ea.entmax_attn_decode_cache4(q.cuda(), cache, i32([ids]), i32([n]), 1.5, page)
+    check_decode(q, [ks], [vs], 1.5, *(t.cpu() for t in got), "bf16")
+
+
+def test_norm_rope_beyond_two_gigabytes(ea):
+    # the last tokens of 262144 with 66 rows each: 4.4 GB in and out
+    N, Hq, Hk, d = 262144, 64, 2, 128
+    rows = torch.randn(1, N, Hq + Hk, d, device="cuda", dtype=torch.bfloat16, generator=torch.Generator(device="cuda").manual_seed(51))
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")[None]
+    freq = torch.rand(d // 2, generator=torch.Generator().manual_seed(52))
+    q, k = ea.entmax_attn_qk_norm_rope_fwd(rows[:, :, :Hq], rows[:, :, Hq:], pos, freq.cuda())
+    assert rows.numel() > 2 ** 31                                   # (elements; q_out has 2 ** 32 bytes)
+    cos, sin = ref.rotation(pos[None, :, -3:].cpu(), freq, [d // 2])
+    for y, x in ((q, rows[:, -3:, :Hq]), (k, rows[:, -3:, Hq:])):
+        want = ref.prep(x.cpu().double(), None, cos, sin, False, 1e-6, True)
+        err = (y[:, :, -3:].cpu().double() - want).abs()
+        assert (err <= 2.0 ** -8 * want.abs() * 1.01 + 20 * U * pair_norms(want.abs(), d, False) * 2 + 1e-37).all()
+    dy = torch.randn(1, Hq, N, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(53))
+    dk = torch.zeros(1, Hk, N, d, device="cuda")
+    dq = ea.entmax_attn_qk_norm_rope_bwd(rows[:, :, :Hq], rows[:, :, Hq:], dy, dk, pos, freq.cuda())[0]
+    part = ea.entmax_attn_qk_norm_rope_bwd(rows[:, -3:, :Hq], rows[:, -3:, Hq:], dy[:, :, -3:].contiguous(), dk[:, :, -3:].contiguous(),
+                                           pos[:, -3:].contiguous(), freq.cuda())[0]
+    assert torch.equal(dq[:, -3:], part)
