@@ -37,7 +37,7 @@ struct Cache4Params {
     float* O; float* tau; int32_t* support;
     float* scores;            // [R][Hq][stride]: s_j, where a block's maximum was in the window (else whatever stood there)
     float* bmax;              // [R][Hq][stride / 64]: maximum of 64 keys; +inf also where a score is not a number or a page id out of range
-    long stride;              // keys a head has room for: max_len rounded up to 64
+    long stride;              // keys a head has room for (cache4_stride)
     int part;                 // keys per wave of the score kernel, a multiple of 64
     int R, Hq, Hk, G, colgroups;        // G = Hq / Hk query heads per key head, in colgroups of up to 16
     int blocks, n_pages, page_shift, max_len;
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
     // the waves take the work-group's blocks in turn, so that a request shorter than its part of the keys is all four waves' work
     const int c0 = chunk * C4_WAVES * p.part;
     auto block_key = [&](int i) { return c0 + (i * C4_WAVES + wave) * C4_BLOCK; };        // first key of the wave's block i
-    const bool live = cg * 16 + col < p.G;
+    const bool live = cg * 16 + col < p.G;                  // (else a column without a head: zeros, nothing is written)
     const long head = (long)req * p.Hq + kvh * p.G + (live ? cg * 16 + col : 0);
     // length, pages and query are asked for together, and the first keys before the query is worked on.  Lane 4 i + j: the sixteen
     // keys j of block i (C4_MAX_PART: at most eight blocks).

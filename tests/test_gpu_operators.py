@@ -390,6 +390,10 @@ DECODE = [
     ([5000], 2, 2, 128, "f32", 32, 1.1, 1.0),                  # r = 10: hundreds of keys in the support
     ([3000], 2, 1, 64, "bf16", 16, 1.02, 1.5),                 # r = 50
     ([2000], 2, 1, 128, "f32", 16, 1.004, 1.5),                # r = 250
+    ([100, 0, 1000, 17], 8, 1, 64, "f32", 16, 1.5, 1.5),       # eight heads side by side twice, and one more than that
+    ([100, 1000], 9, 1, 64, "bf16", 32, 1.75, 1.5),
+    ([7 * i for i in range(40)], 16, 2, 64, "bf16", 64, 1.5, 1.5),             # 640 heads: four waves each in the second kernel
+    ([33 * i for i in range(1, 34)], 16, 1, 128, "bf16", 32, 1.25, 1.0),
     ([70000], 8, 2, 64, "bf16", 128, 1.5, 1.5),
 ]
 
