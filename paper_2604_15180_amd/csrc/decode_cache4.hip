@@ -293,16 +293,20 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 }
 
 // A wave takes a part of the head's blocks, in order, and keeps its candidates to itself: the waves meet only in the sums of an
-// evaluation and of the output.
-template <int D, int AM, int NW>
+// evaluation and of the output.  SPLIT work-groups do the same for a head, each for a part of the output's elements: with few heads the
+// card is empty, and what one CU can have on its way limits how fast the rows of a long support are read (32 heads of 131072 keys at
+// alpha 1.05: 1726 us with one, 593 with four; flat heads at alpha 1.5: 203 and 175; short supports the same; 256 heads of 1000 keys
+// 7.2 and 12.9).
+template <int D, int AM, int NW, int SPLIT>
 __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) {
-    constexpr int SEG = 512, ROW = D / 2, SROW = D / 32, LPR = D / 8, AT_ONCE = 64 / LPR, U = 4;
+    constexpr int SEG = 512, ROW = D / 2, SROW = D / 32, DS = D / SPLIT, LPR = DS / 8, AT_ONCE = 64 / LPR, U = 4;
     __shared__ float lx[NW][SEG];           // c (s - s_max), in the order of the keys; then the probabilities
     __shared__ int lj[NW][SEG];             // key; then its slot
     __shared__ float red[2][NW][2];
     __shared__ int ired[NW];
-    __shared__ float osum[NW][D];
+    __shared__ float osum[NW][DS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int slice = blockIdx.z;             // elements DS * slice .. of the output
     const int h = blockIdx.x, req = blockIdx.y, kvh = h / p.G;
     const long head = (long)req * p.Hq + h;
     const int len = p.lens[req];
@@ -320,16 +324,17 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) gm = fmaxf(gm, red[0][w][0]);
-    float* O = p.O + head * D;
+    float* O = p.O + head * D + slice * DS;
     if (len == 0 || !len_ok || !(fabsf(gm) < INFINITY)) {
         // no keys: zeros.  A length or page out of range, or a score that is infinite or not a number: not a number
         const float v = len == 0 ? 0.f : __builtin_nanf("");
-        for (int i = tid; i < D; i += 64 * NW) O[i] = v;
-        if (tid == 0) { p.tau[head] = v; if (p.support) p.support[head] = len == 0 ? 0 : -1; }
+        if (tid < DS) O[tid] = v;
+        if (tid == 0 && slice == 0) { p.tau[head] = v; if (p.support) p.support[head] = len == 0 ? 0 : -1; }
         return;
     }
     // f(x, key) for the scores of the wave's blocks that reach into the window, in the order of their keys, a block at a time, four
-    // such loads in flight, and then after().  (The score kernel has written these blocks: its window was this one or a lower one.)
+    // such loads in flight, until after() says that it is enough.  (The score kernel has written these blocks: its window was this one
+    // or a lower one.)
     auto walk = [&](auto f, auto after) {
         for (int c0 = b0; c0 < b1; c0 += 64) {
             unsigned long long todo = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (key[u] >= 0) f(p.c * (s[u] - gm), key[u] + lane);       // (keys past the end were written as -inf)
-                after();
+                if (after()) return;
             }
         }
     };
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         const int at = total + __popcll(in & ((1ull << lane) - 1ull));
         if (x >= -1.f && at < SEG) { lx[wave][at] = x; lj[wave][at] = j; }
         total += __popcll(in);
-    }, [] {});
+    }, [&] { return total > SEG; });
     const bool over = total > SEG;          // then every evaluation of this wave streams its blocks instead
     // F = sum [x - tau]^r and G = sum [x - tau]^(r - 1) over the work-group, the same in every thread
     int turn = 0;
@@ -429,9 +434,9 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
     }
 
     // o = sum over the support of p_j v_j.  The support is moved to the front of the wave's candidates, with slots in place
-    // of keys; then a row of values is D / 8 lanes with eight each, and a wave reads 64 / (D / 8) rows at a time.
+    // of keys; then a row's part of values is DS / 8 lanes with eight each, and a wave reads 64 / (DS / 8) rows at a time.
     const int32_t* pages = p.table + (long)req * p.blocks;
-    const int shift = p.page_shift, in_page = (1 << shift) - 1, sub = lane % LPR, rsel = lane / LPR;
+    const int shift = p.page_shift, in_page = (1 << shift) - 1, sub = lane % LPR, rsel = lane / LPR, eight = slice * LPR + sub;
     const long page_bytes = (long)(2 * (ROW + SROW)) << shift, stride = page_bytes * p.Hk;
     const unsigned char* const values = p.cache + kvh * page_bytes + ((long)(ROW + SROW) << shift);
     float acc[8];
@@ -461,8 +466,8 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
                     const int slot = lj[wave][i];
                     const unsigned char* vb = values + (slot >> shift) * stride;
                     const int row = slot & in_page;
-                    codes[u] = *(const unsigned int*)(vb + row * ROW + 4 * sub);
-                    const unsigned int byte = vb[(ROW << shift) + row * SROW + (sub >> 2)];
+                    codes[u] = *(const unsigned int*)(vb + row * ROW + 4 * eight);
+                    const unsigned int byte = vb[(ROW << shift) + row * SROW + (eight >> 2)];
                     ps[u] = lx[wave][i] * (byte == 255u ? __builtin_nanf("") : __uint_as_float(byte << 23));
                 }
             }
@@ -485,12 +490,14 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         }
     } else {
         walk([&](float x, int j) { keep_support(x, j, kept); },
-             [&] { if (kept > SEG - 64 * U) { add_rows(kept); kept = 0; } });
+             [&] { if (kept > SEG - 64 * U) { add_rows(kept); kept = 0; } return false; });
     }
     add_rows(kept);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        if constexpr (LPR == 8) acc[k] += dpp_move<0x128>(acc[k]);              // (row_ror 8)
+        if constexpr (LPR <= 8) acc[k] += dpp_move<0x128>(acc[k]);              // (row_ror 8, 4, 2)
+        if constexpr (LPR <= 4) acc[k] += dpp_move<0x124>(acc[k]);
+        if constexpr (LPR <= 2) acc[k] += dpp_move<0x122>(acc[k]);
         acc[k] = across16(acc[k]);
         if (rsel == 0) osum[wave][8 * sub + k] = acc[k];
     }
@@ -498,14 +505,14 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
     turn ^= 1;                              // (a wave may still be reading the last evaluation's sums)
     if (lane == 0) { ired[wave] = nsup; red[turn][wave][0] = psum; }
     __syncthreads();
-    if (tid < D) {
+    if (tid < DS) {
         float o = 0.f, sum = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) { o += osum[w][tid]; sum += red[turn][w][0]; }
         // the p add up to 1 but for tau's last place, r times over: what is left of it is common to all where r is large
         O[tid] = o / sum;
     }
-    if (tid == 0) {
+    if (tid == 0 && slice == 0) {
         p.tau[head] = (float)(p.c64 * (double)gm + (double)tau);
         int sum = 0;
         for (int w = 0; w < NW; ++w) sum += ired[w];
@@ -513,12 +520,12 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
     }
 }
 
-template <int D, int NW> void cache4_entmax(const Cache4Params& p, hipStream_t s) {
-    const dim3 grid(p.Hq, p.R), block(64 * NW);
+template <int D, int NW, int SPLIT> void cache4_entmax(const Cache4Params& p, hipStream_t s) {
+    const dim3 grid(p.Hq, p.R, SPLIT), block(64 * NW);
     switch (p.alpha == 1.5f ? ALPHA_15 : p.alpha == 2.0f ? ALPHA_20 : ALPHA_GEN) {
-        case ALPHA_15: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_15, NW>), grid, block, 0, s, p); break;
-        case ALPHA_20: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_20, NW>), grid, block, 0, s, p); break;
-        default: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_GEN, NW>), grid, block, 0, s, p); break;
+        case ALPHA_15: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_15, NW, SPLIT>), grid, block, 0, s, p); break;
+        case ALPHA_20: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_20, NW, SPLIT>), grid, block, 0, s, p); break;
+        default: hipLaunchKernelGGL((cache4_entmax_kernel<D, ALPHA_GEN, NW, SPLIT>), grid, block, 0, s, p); break;
     }
 }
 template <class E, int D>
@@ -527,7 +534,10 @@ void cache4_run(const Cache4Params& p, hipStream_t s) {
     const dim3 grid(p.Hk * p.colgroups, p.R, (p.max_len + per_group - 1) / per_group), block(64 * C4_WAVES);
     if (D == 64 && p.G <= 8) hipLaunchKernelGGL((cache4_scores_kernel<E, D, D == 64>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((cache4_scores_kernel<E, D, false>), grid, block, 0, s, p);
-    if ((long)p.R * p.Hq < 512) cache4_entmax<D, 8>(p, s); else cache4_entmax<D, 4>(p, s);
+    const long heads = (long)p.R * p.Hq;
+    if (heads <= 64) cache4_entmax<D, 8, 4>(p, s);
+    else if (heads < 512) cache4_entmax<D, 8, 1>(p, s);
+    else cache4_entmax<D, 4, 1>(p, s);
 }
 
 }  // namespace ea
