@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 // A wave takes a part of the head's blocks, in order, and keeps its candidates to itself: the waves meet only in the sums of an
 // evaluation and of the output.  SPLIT work-groups do the same for a head, each for a part of the output's elements: with few heads the
 // card is empty, and what one CU can have on its way limits how fast the rows of a long support are read (32 heads of 131072 keys at
-// alpha 1.05: 1726 us with one, 593 with four; flat heads at alpha 1.5: 203 and 175; short supports the same; 256 heads of 1000 keys
+// alpha 1.05: 1726 us with one, 566 with four; flat heads at alpha 1.5: 203 and 149; short supports the same; 256 heads of 1000 keys
 // 7.2 and 12.9).
 template <int D, int AM, int NW, int SPLIT>
 __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) {
@@ -333,9 +333,9 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         return;
     }
     // f(x, key) for the scores of the wave's blocks that reach into the window, in the order of their keys, a block at a time, four
-    // such loads in flight, until after() says that it is enough.  (The score kernel has written these blocks: its window was this one
-    // or a lower one.)
-    auto walk = [&](auto f, auto after) {
+    // such loads in flight, and then after(); every 64 blocks enough() may end it (asked after every load, 1 us more for 48 requests up
+    // to 32768 keys).  (The score kernel has written these blocks: its window was this one or a lower one.)
+    auto walk = [&](auto f, auto after, auto enough) {
         for (int c0 = b0; c0 < b1; c0 += 64) {
             unsigned long long todo = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
             while (todo) {
@@ -352,8 +352,9 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (key[u] >= 0) f(p.c * (s[u] - gm), key[u] + lane);       // (keys past the end were written as -inf)
-                if (after()) return;
+                after();
             }
+            if (enough()) return;
         }
     };
     // The same for sums alone: g(x) for all of them, 256 keys a load.
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         const int at = total + __popcll(in & ((1ull << lane) - 1ull));
         if (x >= -1.f && at < SEG) { lx[wave][at] = x; lj[wave][at] = j; }
         total += __popcll(in);
-    }, [&] { return total > SEG; });
+    }, [] {}, [&] { return total > SEG; });
     const bool over = total > SEG;          // then every evaluation of this wave streams its blocks instead
     // F = sum [x - tau]^r and G = sum [x - tau]^(r - 1) over the work-group, the same in every thread
     int turn = 0;
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         }
     } else {
         walk([&](float x, int j) { keep_support(x, j, kept); },
-             [&] { if (kept > SEG - 64 * U) { add_rows(kept); kept = 0; } return false; });
+             [&] { if (kept > SEG - 64 * U) { add_rows(kept); kept = 0; } }, [] { return false; });
     }
     add_rows(kept);
 #pragma unroll
