@@ -365,7 +365,10 @@ def _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sectio
 
 
 def _row_strides(t):
-    return _ThreeStrides(*t.stride()[:3])
+    a, b, c, _ = t.stride()
+    if (a | b | c) & 7:     # (of a dimension of one torch keeps any stride; no row is a step along it away)
+        a, b, c = (0 if n == 1 else s for n, s in zip(t.shape, (a, b, c)))
+    return _ThreeStrides(a, b, c)
 
 
 def entmax_attn_qk_norm_rope_fwd(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, norm=True, sections=None,
@@ -458,13 +461,20 @@ def _cache_args(call, cache, d, page_size):
     return cache.shape[0], cache.shape[1]
 
 
+def _token_strides(t):
+    a, b, _ = t.stride()
+    if (a | b) & 7:         # (as in _row_strides)
+        a, b = (0 if n == 1 else s for n, s in zip(t.shape, (a, b)))
+    return _TwoStrides(a, b)
+
+
 def _cache_rows(call, k, v, slots, Hk):
     if k.dim() != 3 or k.shape != v.shape or k.shape[1] != Hk or k.dtype != v.dtype:
         raise ValueError(f"{call}: K, V must be [T,Hk,d] of one dtype, with the cache's Hk")
     if k.numel() and (k.stride(2) != 1 or v.stride(2) != 1):
         raise ValueError(f"{call}: the elements of a row must be contiguous")
     _int32(call, "slots", slots, (k.shape[0],))
-    return _TwoStrides(*k.stride()[:2]), _TwoStrides(*v.stride()[:2])
+    return _token_strides(k), _token_strides(v)
 
 
 def entmax_attn_cache4_write(K, V, slots, cache, page_size):

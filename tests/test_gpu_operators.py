@@ -309,6 +309,30 @@ def test_cache_rows_none_and_zero_page(ea):
     assert (k == 0).all() and (v == 0).all()
 
 
+def test_strides_of_dimensions_of_one(ea):
+    """A channels-first layer's output of one token: torch leaves the dimension of one a stride that no row could have."""
+    g = torch.Generator().manual_seed(8)
+    x = torch.randn(6, 64, 1, generator=g).cuda().transpose(1, 2)                # [6,1,64], strides 64, 1, 1
+    assert x.stride() == (64, 1, 1)
+    slots, cache, same = i32([3, 9, 0, 17, 31, 8]), ea.entmax_attn_cache4_empty(2, 1, 64, 16), ea.entmax_attn_cache4_empty(2, 1, 64, 16)
+    ea.entmax_attn_cache4_write(x, x, slots, cache, 16)
+    y = torch.empty(6, 1, 64, device="cuda").copy_(x)
+    ea.entmax_attn_cache4_write(y, y, slots, same, 16)
+    assert torch.equal(cache, same)
+    out = [torch.full((6, 64, 1), 3.0, device="cuda").transpose(1, 2) for _ in range(2)]
+    ea.entmax_attn_cache4_read(cache, slots, 16, 64, out=out)
+    for a, b in zip(out, ea.entmax_attn_cache4_read(cache, slots, 16, 64, torch.float32)):
+        assert torch.equal(a, b)
+    q, r = x.as_strided((6, 1, 1, 64), (64, 1, 3, 1)), y.view(6, 1, 1, 64)
+    pos, freq, dy = i32([[5]] * 6), torch.rand(32, generator=g).cuda(), torch.randn(6, 1, 1, 64, generator=g).cuda()
+    for a, b in zip(ea.entmax_attn_qk_norm_rope_fwd(q, q, pos, freq), ea.entmax_attn_qk_norm_rope_fwd(r, r, pos, freq)):
+        assert torch.equal(a, b)
+    grads = [torch.empty(6 * 64, device="cuda").as_strided((6, 1, 1, 64), (64, 1, 3, 1)) for _ in range(2)]
+    ea.entmax_attn_qk_norm_rope_bwd(q, q, dy, dy, pos, freq, out=grads)
+    for a, b in zip(grads, ea.entmax_attn_qk_norm_rope_bwd(r, r, dy, dy, pos, freq)):
+        assert torch.equal(a, b)
+
+
 # ---- decode from the cache ----------------------------------------------------------------------------------------
 
 def make_cache(ea, lens, Hk, d, page, sigma, seed, keys=None, spare=3):
