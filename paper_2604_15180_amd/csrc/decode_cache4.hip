@@ -417,7 +417,8 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
             const float over1 = AM == ALPHA_15 ? sqrtf(F) - 1.f : AM == ALPHA_20 ? F - 1.f
                                 : r <= 16.f    ? __builtin_amdgcn_exp2f(__builtin_amdgcn_logf(F) * (1.f / r)) - 1.f
                                                : expm1f(logf(F) / r);
-            const float next = fminf(tau + over1 * F / ((over1 + 1.f) * G), 0.f);
+            // (N keys: 1 = F <= N (-tau)^r, so that tau <= -2^-22 for the 2^22 keys there can be; rounding must not carry it to 0)
+            const float next = fminf(tau + over1 * F / ((over1 + 1.f) * G), -0x1p-23f);
             if (!(next > tau)) break;
             const bool small = next - tau < 3e-8f;
             tau = next;

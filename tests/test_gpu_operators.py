@@ -479,6 +479,22 @@ def test_decode_marks_what_it_cannot_answer(ea):
     assert torch.isfinite(got[0]).all()
 
 
+@pytest.mark.parametrize("alpha", [1.5, 1.9999, 2.0, 3.0])
+def test_decode_of_the_longest_request_with_equal_scores(ea, alpha):
+    """2^22 keys of zero, one page serving for all: tau = -N^(-1/r), as close to the maximum as it can be, and every p = 1/N."""
+    N, r = 1 << 22, 1 / (alpha - 1)
+    cache = ea.entmax_attn_cache4_empty(1, 1, 64, 256)
+    ea.entmax_attn_cache4_write(torch.zeros(256, 1, 64, device="cuda"), torch.ones(256, 1, 64, device="cuda"), i32(list(range(256))), cache, 256)
+    table = torch.zeros(1, N // 256, dtype=torch.int32, device="cuda")
+    O, tau, support = ea.entmax_attn_decode_cache4(torch.ones(1, 1, 64, device="cuda"), cache, table, i32([N]), alpha, 256)
+    # a lane adds up to N / 8 / 32 of the output's terms and N / 8 / 64 of the p and of the solve's, then 64 over lanes and waves;
+    # F = N (-tau)^r: an error of F is r times tau's relative one.  The solve ends where a step is below 3e-8 (or 26 halvings)
+    assert (support == N).all()
+    assert ((O - 1).abs() <= (N // 256 + N // 512 + 64) * U).all(), O
+    want = -float(N) ** (-1 / r)
+    assert (tau.double().cpu() - want).abs().item() <= abs(want) * (N // 512 + 64) * U / r + 6e-8, (tau, want)
+
+
 def test_decode_agrees_with_the_decode_of_a_contiguous_cache(ea):
     R, H, n, d, page = 2, 4, 777, 128, 64
     cache, table, ln, ks, vs = make_cache(ea, [n] * R, H, d, page, 1.5, seed=33)
