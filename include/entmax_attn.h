@@ -328,6 +328,7 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or five (float32) 8-bit terms: a bf16
  * element is exact down to 2^-12 of the largest of its row and known to 2^-20 of that below, a float32 element is exact down to
  * 2^-6 and known to 2^-30 (rows whose largest element is below 2^-100 lose more); the rest is in float32.
+ * A probability is the power r = 1 / (alpha - 1) of a float32 difference: with alpha next to 1 it is known to about r 2^-21 of it.
  * Results repeat bit for bit.  Two calls at once need two workspaces.
  */
 size_t entmax_attn_cache4_page_bytes(int Hk, int d, int page_size);      /* 0 for a bad shape */

@@ -479,6 +479,26 @@ def test_decode_marks_what_it_cannot_answer(ea):
     assert torch.isfinite(got[0]).all()
 
 
+@pytest.mark.parametrize("alpha", [1.001, 1.0001, 1.00001])
+def test_decode_with_alpha_next_to_one(ea, alpha):
+    """r = 1 / (alpha - 1) is the power of the probabilities, up to 1e5 here: y is rounded by 2 u, its logarithm (log2, 2^-22 at the
+    most) by 4 u, the exponent of up to 64 by 64 u; a score's error d u sum |q k| counts 1 / sqrt(d) each in p and in
+    the largest score.  The sum of the p that O is divided by doubles it all."""
+    from oracle import entmax_oracle as eo
+    alpha = float(np.float32(alpha))
+    r, d = 1 / (alpha - 1), 64
+    cache, table, lens, ks, vs = make_cache(ea, [1500], 1, d, 32, 1.0, 17)
+    q = torch.randn(1, 2, d, generator=torch.Generator().manual_seed(5))
+    O, tau, support = ea.entmax_attn_decode_cache4(q.cuda(), cache, table, lens, alpha, 32)
+    K, V = (np.repeat(x[0].transpose(1, 0, 2), 2, 0)[None] for x in (ks, vs))
+    want = eo.attn_decode(q.double().numpy(), K, V, alpha)
+    ds = d * U * (np.abs(K[0]) @ np.abs(q[0].double().numpy())[..., None]).max() + 2.0 ** -30 * np.abs(K).sum(-1).max() * q.abs().max().item()
+    tol = 2 * (6 * r * U + (64 + 24) * U + 2 * ds / np.sqrt(d))
+    err = np.abs(O[0].double().cpu().numpy() - want["O"][0]) / np.einsum("hn,hnd->hd", want["P"][0], np.abs(V[0]))
+    assert (err <= tol).all(), (err.max(), tol)
+    print("  of allowed", err.max() / tol, flush=True)
+
+
 @pytest.mark.parametrize("alpha", [1.5, 1.9999, 2.0, 3.0])
 def test_decode_of_the_longest_request_with_equal_scores(ea, alpha):
     """2^22 keys of zero, one page serving for all: tau = -N^(-1/r), as close to the maximum as it can be, and every p = 1/N."""
