@@ -118,8 +118,11 @@ EA_DEV int query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], flo
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             constexpr float EIGHTHS = 1.5f * (1 << 20);          // added and taken off again: rounds to multiples of 1/8
-            int bits = __builtin_amdgcn_cvt_pk_fp8_f32((v[0] + EIGHTHS) - EIGHTHS, (v[1] + EIGHTHS) - EIGHTHS, 0, false);
-            bits = __builtin_amdgcn_cvt_pk_fp8_f32((v[2] + EIGHTHS) - EIGHTHS, (v[3] + EIGHTHS) - EIGHTHS, bits, true);
+            // One rounding each: e4m3's own steps are 1/8 and more from 1 on, and below 1 every multiple of 1/8 is an e4m3 value.  (To
+            // 1/8 first everywhere, what is left may pass half a step of e4m3, and the next terms do not catch up with it.)
+            auto rounded = [](float x) { return fabsf(x) < 1.f ? (x + EIGHTHS) - EIGHTHS : x; };
+            int bits = __builtin_amdgcn_cvt_pk_fp8_f32(rounded(v[0]), rounded(v[1]), 0, false);
+            bits = __builtin_amdgcn_cvt_pk_fp8_f32(rounded(v[2]), rounded(v[3]), bits, true);
             words[t][4 * run + wave][lane] = bits;
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(bits, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(bits, true);
             v[0] = (v[0] - lo[0]) * 32.f; v[1] = (v[1] - lo[1]) * 32.f;
