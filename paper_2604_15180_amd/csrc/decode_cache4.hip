@@ -395,7 +395,11 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         float f = 0.f, gs = 0.f;
         auto term = [&](float x) {
             const float y = x - tau;
-            if (y > 0.f) { const float y1 = pow_r1<AM>(y, r); gs += y1; f = fmaf(y1, y, f); }
+            if (!(y > 0.f)) return;
+            if (AM == ALPHA_GEN && r < 1.f) { f += pow_r<AM>(y, r); return; }       // (pow_r1 holds y at 1e-6 and above there; G is not asked for)
+            const float y1 = pow_r1<AM>(y, r);
+            gs += y1;
+            f = fmaf(y1, y, f);
         };
         if (!over) for (int i = lane; i < total; i += 64) term(lx[wave][i]);
         else stream(term);
@@ -409,7 +413,9 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         for (int w = 0; w < NW; ++w) { F += red[turn][w][0]; G += red[turn][w][1]; }
     };
     // tau in [-1, 0] (Eq. 5).  r >= 1: F^(1/r) is a norm of the [x - tau]_+, convex in tau, so Newton steps for F^(1/r) = 1 from the
-    // left rise to the root and stay left of it; they end where a step no longer moves tau.  r < 1 (alpha > 2): bisection.
+    // left rise to the root and stay left of it; they end where a step no longer moves tau.  r < 1 (alpha > 2): bisection over the
+    // floats from 2^-45 to 1 for -tau, by their bits, since N equal keys have tau = -N^(-1/r), down to 2^-44 (2^22 keys, r = 1/2), and
+    // to be known relative to itself: 29 evaluations, and -tau is the first float at which F >= 1.
     float tau = -1.f;
     if (r >= 1.f) {
         for (int it = 0; it < 40; ++it) {
@@ -428,14 +434,14 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
             if (small) break;
         }
     } else {
-        float lo = -1.f, hi = 0.f;
-        for (int it = 0; it < 26; ++it) {
+        unsigned int lo = __float_as_uint(0x1p-45f), hi = __float_as_uint(1.f);     // F(-lo) < 1 <= F(-hi)
+        while (hi - lo > 1) {
             float F, G;
-            tau = 0.5f * (lo + hi);
-            eval(tau, F, G);
-            if (F >= 1.f) lo = tau; else hi = tau;
+            const unsigned int mid = (lo + hi) >> 1;
+            eval(-__uint_as_float(mid), F, G);
+            if (F >= 1.f) hi = mid; else lo = mid;
         }
-        tau = 0.5f * (lo + hi);
+        tau = -__uint_as_float(hi);
     }
 
     // o = sum over the support of p_j v_j.  The support is moved to the front of the wave's candidates, with slots in place

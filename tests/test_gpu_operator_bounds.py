@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import operators_ref as ref
 from tests.test_gpu_operators import DT, U, ea, i32  # noqa: F401  (ea: the fixture)
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +44,59 @@ def test_decode_scores_of_single_elements(ea, dtype, exact, known, d, G):  # noq
     tol = np.abs(want) * U + np.where(np.abs(x) < exact * top, known * top * scale, 0.0) + 2.0 ** -52 * top
     assert (err <= tol).all(), ((err > tol).mean(), (err / tol).max())
     assert (O == 1).all() and (support == 1).all()
+
+
+# ---- alpha above 2 ------------------------------------------------------------------------------------------------
+
+
+def near_ties(ea, alpha, counts, delta):  # noqa: F811
+    """256 * counts[j] keys with the score -LEVELS[j] * delta, with values of 2^j: what the decode gives, and the
+    definition's tau, weights of a key of each level and x in 64 bits."""
+    page, d, r = 256, 64, 1 / (alpha - 1)
+    n, level = 256 * np.array(counts, dtype=np.float64), ref.LEVELS[:len(counts)]
+    k, v = torch.zeros(len(counts), page, 1, d), torch.zeros(len(counts), page, 1, d)
+    k[..., 0] = -torch.from_numpy(level).float()[:, None, None]
+    k[..., 1] = 6                                                               # (so that all blocks have the scale 1; its query element is 0)
+    v[:] = 2.0 ** torch.arange(len(counts))[:, None, None, None]
+    cache = ea.entmax_attn_cache4_empty(len(counts), 1, d, page)
+    ea.entmax_attn_cache4_write(k.flatten(0, 1).cuda(), v.flatten(0, 1).cuda(), i32(list(range(256 * len(counts)))), cache, page)
+    table = torch.repeat_interleave(torch.arange(len(counts)), torch.tensor(counts)).to(torch.int32)[None].cuda()
+    q = torch.zeros(1, 1, d)
+    q[0, 0, 0] = delta = float(np.float32(delta))
+    got = ea.entmax_attn_decode_cache4(q.cuda(), cache, table, i32([int(n.sum())]), alpha, page)
+    x = -(alpha - 1) / 8 * delta * level
+    lo, hi = 0.0, 1.0                                                           # of -tau
+    for _ in range(200):
+        mid = (lo + hi) / 2
+        lo, hi = (mid, hi) if (n * np.maximum(x + mid, 0) ** r).sum() < 1 else (lo, mid)
+    return got, n, x, hi, r
+
+
+def check_near_ties(got, n, x, t, r):
+    """What a solve in fp32 may be off by: a power is 2^(r log2 y), the logarithm to 2^-23 of itself, the product to 2^-24, the power to
+    2^-22; x to 4 u of itself; sums of N / 512 terms a lane and 64 over lanes and waves.  F grows with t at least as t^r does."""
+    O, tau, support = got
+    total = n.sum()
+    y = x + t
+    L = max(abs(np.log2(y[y > 0]))) * r
+    power = 0.7 * L * (2.0 ** -23 + 2.0 ** -24) + 2.0 ** -22
+    dt = (power + (total / 512 + 64) * U) / r * t + 5 * U * t
+    assert abs(tau.item() + t) <= dt, (tau.item(), -t, dt)
+    dy = dt + 4 * U * abs(x)
+    p = lambda y: np.maximum(y, 0) ** r                                         # noqa: E731
+    v = 2.0 ** np.arange(len(n))
+    dp = np.maximum(p(y + dy) - p(y), p(y) - p(y - dy)) + power * p(y)
+    want = (n * p(y) * v).sum() / (n * p(y)).sum()
+    tol = (n * dp * abs(v - want)).sum() / (n * p(y)).sum() * 1.1 + 2 * want * (total / 256 + 96) * U
+    assert (O[0, 0] - want).abs().max() <= tol, (O[0, 0, 0].item(), want, tol)
+    assert n[y > dy].sum() <= support.item() <= n[y > -dy].sum()
+
+
+@pytest.mark.parametrize("alpha", [2.25, 2.5, 3.0])
+@pytest.mark.parametrize("n,m,at", [(8, 1, 1.5), (8, 1, 0.5), (40, 2, 1.02), (40, 2, 0.97), (1200, 5, 1.5), (1200, 500, 0.8), (15700, 300, 0.5)])
+def test_decode_threshold_of_near_ties_with_alpha_above_two(ea, n, m, at, alpha):  # noqa: F811
+    """256 n keys with the largest score, and others `at` and twice `at` times as far below it as the threshold of the former
+    alone, N^-(alpha - 1) down to 6e-14."""
+    alpha = float(np.float32(alpha))
+    delta = 2 * at * (256.0 * n) ** -(alpha - 1) * 8 / (alpha - 1)                 # (the first level is 0.5)
+    check_near_ties(*near_ties(ea, alpha, [n, m, m], delta))
