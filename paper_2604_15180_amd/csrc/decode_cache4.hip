@@ -413,7 +413,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
         for (int w = 0; w < NW; ++w) { F += red[turn][w][0]; G += red[turn][w][1]; }
     };
     // tau in [-1, 0] (Eq. 5).  r >= 1: F^(1/r) is a norm of the [x - tau]_+, convex in tau, so Newton steps for F^(1/r) = 1 from the
-    // left rise to the root and stay left of it; they end where a step no longer moves tau.  r < 1 (alpha > 2): bisection over the
+    // left rise to the root; they end where a step no longer moves tau.  r < 1 (alpha > 2): bisection over the
     // floats from 2^-45 to 1 for -tau, by their bits, since N equal keys have tau = -N^(-1/r), down to 2^-44 (2^22 keys, r = 1/2), and
     // to be known relative to itself: 29 evaluations, and -tau is the first float at which F >= 1.
     float tau = -1.f;
@@ -428,10 +428,11 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
                                                : expm1f(logf(F) / r);
             // (N keys: 1 = F <= N (-tau)^r, so that tau <= -2^-22 for the 2^22 keys there can be; rounding must not carry it to 0)
             const float next = fminf(tau + over1 * F / ((over1 + 1.f) * G), -0x1p-23f);
-            if (!(next > tau)) break;
-            const bool small = next - tau < 3e-8f;
+            // A step from far left may be rounded past the root by some 1e-7; what is left of -tau, down to 2^-22, decides whether that
+            // matters.  From the right a step falls to the left of the root again.
+            const float part = -0x1p-12f * next;
+            if (next > tau ? next - tau < fminf(3e-8f, part) : !(tau - next > part)) { tau = fmaxf(tau, next); break; }
             tau = next;
-            if (small) break;
         }
     } else {
         unsigned int lo = __float_as_uint(0x1p-45f), hi = __float_as_uint(1.f);     // F(-lo) < 1 <= F(-hi)

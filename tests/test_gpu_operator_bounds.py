@@ -100,3 +100,16 @@ def test_decode_threshold_of_near_ties_with_alpha_above_two(ea, n, m, at, alpha)
     alpha = float(np.float32(alpha))
     delta = 2 * at * (256.0 * n) ** -(alpha - 1) * 8 / (alpha - 1)                 # (the first level is 0.5)
     check_near_ties(*near_ties(ea, alpha, [n, m, m], delta))
+
+
+# ---- long supports ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("alpha,counts,delta", [
+    (1.95, [1006, 88, 9, 2, 11, 2, 5171, 4557], 1.5118186e-06), (1.95, [1010, 1, 333, 1020, 91, 295, 6609, 3829], 3.0919838e-07),
+    (1.97, [1006, 190, 1, 98, 27, 2947, 1, 5965], 1.5801573e-06), (1.97, [3159, 3583, 12, 258, 6700, 62, 132, 36], 5.305047e-07),
+    (1.99, [3160, 624, 85, 62, 23, 3, 7517, 90], 2.9965974e-07), (2.0, [3160, 624, 85, 62, 23, 3, 7517, 90], 2.9965974e-07),
+    (2.0, [31, 7, 2, 40], 3e-4), (1.9, [100, 20, 30, 1, 1, 40], 2e-4), (1.75, [9000, 500, 3000], 2e-4)])
+def test_decode_threshold_of_many_near_ties(ea, alpha, counts, delta):  # noqa: F811
+    """Thousands to millions of keys within 1e-4 to 1e-6 of the largest score: -tau is itself of that size, and the first step of the
+    solve, from -1, is known to 2^-24 of 1."""
+    check_near_ties(*near_ties(ea, float(np.float32(alpha)), counts, delta))
