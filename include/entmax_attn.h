@@ -323,8 +323,9 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  *   max_len          at least the largest length, at most 2^22 and max_blocks * page_size: the launch and the workspace go by it
  * A request of length 0 gets O = 0, tau = 0, support 0.  One whose length is negative or above max_len, or that has a
  * page id outside 0 .. n_pages - 1 among the pages it attends to, gets NaN and support -1, and so does a head whose query or
- * keys hold an infinity or a NaN (keys and queries whose products could pass 2^100 count as infinite, for all heads of that
- * key head).  What the cache holds behind a request's last token has no effect.
+ * keys hold an infinity or a NaN, or where 2^floor(log2 max|q|) of the head's query times the scale of a block of its keys
+ * reaches 2^109 (a score might then pass 2^120).  What other heads hold, and the cache behind a request's last token, has no
+ * effect.
  * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or five (float32) 8-bit terms: a bf16
  * element is exact down to 2^-12 of the largest of its row and known to 2^-20 of that below, a float32 element is exact down to
  * 2^-6 and known to 2^-30 (rows whose largest element is below 2^-100 lose more); the rest is in float32.

@@ -90,7 +90,7 @@ template <class E, int D> struct QRow {
     }
 };
 // The waves of a work-group convert their quarters and hand them round through LDS.  Every thread calls this.  Returns the scale byte
-// of keys from which a score of some row may pass 2^120; odd: the lane's row holds an infinity or a NaN.
+// of keys from which a score of the lane's row may pass 2^120; odd: that row holds an infinity or a NaN.
 template <class E, int D, int NT>
 EA_DEV int query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], float (*tops)[16], QTerms<NT>& out, bool& odd) {
     constexpr int RUNS = D / 64;
@@ -138,7 +138,7 @@ EA_DEV int query_terms(const QRow<E, D>& row, int wave, int (*words)[8][64], flo
     }
     // |score| < D * 6 * 2^(byte - 127) * 2^(7 + e) <= 2^(byte - 110 + e)
     odd = !(top < INFINITY);
-    return min(255, 230 - wave_max(odd ? -200 : e));
+    return odd ? 255 : min(255, 230 - e);
 }
 
 EA_DEV unsigned int c4_ordered(float f) {
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
         x.sc[u] = scales[lsrow];
     };
     QTerms<NT> q;
-    int limit;                                              // scale bytes from which a score may not be finite
+    int limit, lowest;                                      // scale bytes from which the lane's, some lane's score may not be finite
     bool odd;                                               // the lane's query is not
     float lmax = -INFINITY;
     auto compute = [&](auto more, Batch& x, int i) {
@@ -255,7 +255,8 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
                 }
         if constexpr (PAIR) best = fmaxf(best, dpp_move<0x128>(best));          // (row_ror 8: the head's other column)
         best = across16_max(best);
-        if (__any(top >= limit) || bad || odd) best = INFINITY;
+        if (bad || odd) best = INFINITY;
+        if (__any(top >= lowest)) { if (wave_max(top) >= limit) best = INFINITY; }     // (hardly ever: a head goes by its own query alone)
         if (!live) best = -INFINITY;
         const float shared_max = c4_from_ordered(__hip_atomic_load(&smax[col], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         lmax = fmaxf(lmax, best);
@@ -280,6 +281,7 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 #pragma unroll
     for (int u = 0; u < U; ++u) if (mine > 1) load(x1, 1, u);
     limit = query_terms<E, D, NT>(qrow, wave, words, tops, q, odd);
+    lowest = -wave_max(-limit);
     if constexpr (PAIR) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)

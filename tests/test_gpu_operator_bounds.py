@@ -113,3 +113,26 @@ def test_decode_threshold_of_many_near_ties(ea, alpha, counts, delta):  # noqa: 
     """Thousands to millions of keys within 1e-4 to 1e-6 of the largest score: -tau is itself of that size, and the first step of the
     solve, from -1, is known to 2^-24 of 1."""
     check_near_ties(*near_ties(ea, float(np.float32(alpha)), counts, delta))
+
+
+# ---- scales at the ends of their range ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,dtype,G", [(128, "bf16", 20), (64, "f32", 20), (64, "bf16", 5)])
+def test_decode_limit_of_keys_and_queries(ea, d, dtype, G):  # noqa: F811
+    """A head is infinite where the power of two in its query's largest element times a key's scale reaches 2^109; whatever the
+    heads beside it hold.  Head h of the queries has its largest element in [2^h, 2^(h+1)); the request's keys have the scale 2^(109 - h0)."""
+    heads = torch.arange(G, dtype=torch.float64)
+    q = torch.zeros(1, G, d, dtype=torch.float64)
+    q[0, :, 5] = 1.75 * torch.exp2(heads)
+    q[0, :, 9] = -torch.exp2(heads)
+    for h0 in (0, 3, G - 1, G):
+        scale = 2.0 ** (109 - h0)
+        k, v = torch.zeros(1, 1, d), torch.ones(1, 1, d)
+        k[0, 0, 5], k[0, 0, 9] = 4 * scale, 2 * scale                                # (4: the largest of a block gets the scale 1)
+        cache, table, lens = one_key_requests(ea, k, v, d)
+        O, tau, support = (x[0].cpu() for x in ea.entmax_attn_decode_cache4(q.to(DT[dtype]).cuda(), cache, table, lens, 2.0, 16))
+        over = heads >= h0
+        assert torch.isnan(O[over]).all() and torch.isnan(tau[over]).all() and (support[over] == -1).all(), h0
+        assert (O[~over] == 1).all() and (support[~over] == 1).all(), h0
+        want = (1.75 * 4 - 2) * torch.exp2(heads) * scale / d ** 0.5                 # (less 1, which is nothing beside it)
+        assert ((tau.double() - want)[~over].abs() <= want[~over] * 2 * U).all(), h0
