@@ -416,7 +416,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
     // floats from 2^-45 to 1 for -tau, by their bits, since N equal keys have tau = -N^(-1/r), down to 2^-44 (2^22 keys, r = 1/2), and
     // to be known relative to itself: 29 evaluations, and -tau is the first float at which F >= 1.
     float tau = -1.f;
-    if (r >= 1.f) {
+    if (AM != ALPHA_GEN || r >= 1.f) {
         for (int it = 0; it < 40; ++it) {
             float F, G;
             eval(tau, F, G);
@@ -427,11 +427,11 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
                                                : expm1f(logf(F) / r);
             // (N keys: 1 = F <= N (-tau)^r, so that tau <= -2^-22 for the 2^22 keys there can be; rounding must not carry it to 0)
             const float next = fminf(tau + over1 * F / ((over1 + 1.f) * G), -0x1p-23f);
-            // A step from far left may be rounded past the root by some 1e-7; what is left of -tau, down to 2^-22, decides whether that
-            // matters.  From the right a step falls to the left of the root again.
-            const float part = -0x1p-12f * next;
-            if (next > tau ? next - tau < fminf(3e-8f, part) : !(tau - next > part)) { tau = fmaxf(tau, next); break; }
+            // (a step from far left may be rounded past the root by some 1e-7: the next one goes back to its left, and what is left
+            // of -tau, down to 2^-22, decides whether it is needed)
+            const float step = next - tau;
             tau = next;
+            if (step < 3e-8f && fabsf(step) <= -0x1p-12f * next) break;
         }
     } else {
         unsigned int lo = __float_as_uint(0x1p-45f), hi = __float_as_uint(1.f);     // F(-lo) < 1 <= F(-hi)
