@@ -326,8 +326,8 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  * keys hold an infinity or a NaN, or where 2^floor(log2 max|q|) of the head's query times the scale of a block of its keys
  * reaches 2^109 (a score might then pass 2^120).  What other heads hold, and the cache behind a request's last token, has no
  * effect.
- * Scores are formed on the matrix cores from the 4-bit keys and q in three (bf16) or five (float32) 8-bit terms: a bf16
- * element is exact down to 2^-12 of the largest of its row and known to 2^-20 of that below, a float32 element is exact down to
+ * Scores are formed on the matrix cores from the 4-bit keys and q in four (bf16) or five (float32) 8-bit terms: a bf16
+ * element is exact down to 2^-17 of the largest of its row and known to 2^-25 of that below, a float32 element is exact down to
  * 2^-6 and known to 2^-30 (rows whose largest element is below 2^-100 lose more); the rest is in float32.
  * A probability is the power r = 1 / (alpha - 1) of a float32 difference: with alpha next to 1 it is known to about r 2^-21 of it.
  * Results repeat bit for bit.  Two calls at once need two workspaces.

@@ -11,8 +11,11 @@
 // exponents (measured: at 2^-14 a product is lost, at any place of the eight; beyond the eight, and for the scales, the sum is fp32's),
 // which a small element's last bits would miss.  The terms lie where e4m3 has the same step, 2^-9, for all small values (below 2^-6 its
 // values are subnormal): codes are multiples of 1/2 up to 6, exponents go up to 2 + 1, and no product has bits below 2^-10.  A term takes
-// five bits off a value's 8 or 24 (four significant ones, and the rest has a sign): three terms hold a bf16 value exactly down to 2^-12
-// of the row's largest, and below that to 2^-20 of it, five an fp32 value down to 2^-6 and to 2^-30.  (Two terms reaching up to 2^8, so with
+// five bits off a value's 8 or 24 (four significant ones, and the rest has a sign): four terms hold a bf16 value exactly down to 2^-17
+// of the row's largest, and below that to 2^-25 of it, five an fp32 value down to 2^-6 and to 2^-30: less than fp32's own rounding of the
+// score.  (Three terms, 2^-12 and 2^-20, were 1 to 3 % faster - one request of 131072 keys 50.8 us, four terms 51.6; 48 requests up to
+// 32768 keys 41.6 and 42.5 - but where one channel of the query is 128 times the others the scores were ten times further off than
+// in fp32.  Two terms reaching up to 2^8, so with
 // smaller last bits beside them, were off by 2e-5 in tau; terms up to 4 by 1e-4 now and then; as they are, the sums are exact up to
 // their one rounding for each term.)
 #include <limits.h>
@@ -154,7 +157,7 @@ EA_DEV float c4_from_ordered(unsigned int u) { return __uint_as_float((u & 0x800
 // formed at once, a lane for each sixteen.
 template <class E, int D, bool PAIR>
 __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Params p) {
-    constexpr int NT = sizeof(typename E::elem) == 2 ? 3 : 5, SETS = 128 / D, TK = 16 * SETS, U = C4_BLOCK / TK;
+    constexpr int NT = sizeof(typename E::elem) == 2 ? 4 : 5, SETS = 128 / D, TK = 16 * SETS, U = C4_BLOCK / TK;
     constexpr int PASSES = PAIR ? 1 : SETS, COLS = PAIR ? 8 : 16;         // instructions of a tile and term; query heads side by side
     static_assert(!PAIR || SETS == 2, "two sets to a tile");
     constexpr int ROW = D / 2, SROW = D / 32;

@@ -21,7 +21,7 @@ def one_key_requests(ea, k, v, d, page=16):  # noqa: F811
 # ---- what a score knows of the query ------------------------------------------------------------------------------
 
 # dtype, exact down to this part of the row's largest element, known to this part below
-TERMS = [("f32", 2.0 ** -6, 2.0 ** -30)]
+TERMS = [("f32", 2.0 ** -6, 2.0 ** -30), ("bf16", 2.0 ** -17, 2.0 ** -25)]
 
 
 @pytest.mark.parametrize("d,G", [(64, 3), (64, 11), (128, 5)])
