@@ -268,8 +268,7 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        // 2^-127 is no normal number: byte 0, which no write leaves, is read through 2^-126 and halved
-        const float scale = byte[u] == 255u ? __builtin_nanf("") : byte[u] == 0u ? 0.5f * __uint_as_float(1u << 23) : __uint_as_float(byte[u] << 23);
+        const float scale = cache4_scale(byte[u]);
         const auto v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 1);
         const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 3);
         const float v[8] = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};

@@ -8,7 +8,12 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "tiles.hpp"
+
 namespace ea {
+
+// The scale of a byte.  (Byte 0, which no write leaves: 2^-127 is subnormal, the bit below the exponent's first.)
+EA_DEV float cache4_scale(unsigned int byte) { return byte == 255u ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 1u << 22); }
 
 constexpr int cache_page_bytes(int d, int page) { return page * 2 * (d / 2 + d / 32); }   // of one head's part
 

@@ -482,7 +482,7 @@ __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) 
                     const int row = slot & in_page;
                     codes[u] = *(const unsigned int*)(vb + row * ROW + 4 * eight);
                     const unsigned int byte = vb[(ROW << shift) + row * SROW + (eight >> 2)];
-                    ps[u] = lx[wave][i] * (byte == 255u ? __builtin_nanf("") : __uint_as_float(byte << 23));
+                    ps[u] = lx[wave][i] * cache4_scale(byte);
                 }
             }
 #pragma unroll

@@ -136,3 +136,23 @@ def test_decode_limit_of_keys_and_queries(ea, d, dtype, G):  # noqa: F811
         assert (O[~over] == 1).all() and (support[~over] == 1).all(), h0
         want = (1.75 * 4 - 2) * torch.exp2(heads) * scale / d ** 0.5                 # (less 1, which is nothing beside it)
         assert ((tau.double() - want)[~over].abs() <= want[~over] * 2 * U).all(), h0
+
+
+def test_decode_and_read_agree_on_the_smallest_scale(ea):  # noqa: F811
+    """Scale byte 0, 2^-127, which no write leaves but a page may hold."""
+    d, page = 64, 16
+    g = torch.Generator().manual_seed(1)
+    cache = ea.entmax_attn_cache4_empty(1, 1, d, page)                          # (all scale bytes 0 or as written)
+    cache.copy_(torch.randint(0, 256, cache.shape, generator=g, dtype=torch.uint8))
+    scales = slice(page * d // 2, page * d // 2 + page * d // 32)
+    cache[0, 0, scales] = 0
+    cache[0, 0, page * d // 2 + page * d // 32:][scales] = 0
+    k, v = ea.entmax_attn_cache4_read(cache, i32([0]), page, d, torch.float32)
+    want = ref.decode_cache(cache.cpu().numpy(), d, page)
+    np.testing.assert_array_equal(k[0, 0].double().cpu().numpy(), want[0][0, 0, 0])
+    np.testing.assert_array_equal(v[0, 0].double().cpu().numpy(), want[1][0, 0, 0])
+    q = torch.zeros(1, 1, d)
+    q[0, 0, 3] = 2.0 ** 108
+    O, tau, _ = ea.entmax_attn_decode_cache4(q.cuda(), cache, i32([[0]]), i32([1]), 2.0, page)
+    assert torch.equal(O[0, 0], v[0, 0])                                        # p = 1
+    assert tau.item() == np.float32(want[0][0, 0, 0, 3] * 2.0 ** 108 / 8 - 1)
