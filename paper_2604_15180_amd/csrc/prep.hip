@@ -69,9 +69,11 @@ template <bool NEIGHBOURS, class T> EA_DEV void store_pairs(T* row, int a, int b
     *(vec*)(row + b) = v;
 }
 
-// cos and sin of the lane's four angles for one token.  The product is formed in 64 bits and whole turns are taken off
-// there: at position 100000 an angle in 32 bits is off by up to 2^-8 of a radian.  What is left, at most half a turn, goes
-// to the hardware's sine and cosine of turns (off by at most 1.3e-7).
+// cos and sin of the lane's four angles for one token.  The product is formed in 64 bits and the nearest quarter turn is taken off
+// there: at position 100000 an angle in 32 bits is off by up to 2^-8 of a radian.  What is left, at most pi / 4, goes to Taylor's series
+// up to its 9th and 10th power (the next terms are below 2e-9 and 2e-10), so that both are known to about a step of fp32 of their
+// own.  (The hardware's sine and cosine of turns are off by 1.3e-7 of 1, and a half turn rounded to fp32 by 9e-8.  They took 4.5 us in
+// place of 4.7 for eight tokens, 44.9 in place of 45.9 for 131072 tokens of three heads; the same for many heads.)
 EA_DEV void angles(const PrepParams& p, int token, int sub, float (&c)[4], float (&s)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -81,10 +83,15 @@ EA_DEV void angles(const PrepParams& p, int token, int sub, float (&c)[4], float
             int ax = 0;
 #pragma unroll
             for (int k = 0; k < MAX_AXES - 1; ++k) ax += i >= p.end[k];
-            const double turns = (double)p.pos[(long)ax * p.tokens + token] * ((double)p.inv_freq[i] * 0.15915494309189533577);
-            const float t = (float)(turns - __builtin_rint(turns));
-            c[e] = __builtin_amdgcn_cosf(t);
-            s[e] = __builtin_amdgcn_sinf(t);
+            const double quarters = (double)p.pos[(long)ax * p.tokens + token] * ((double)p.inv_freq[i] * 0.63661977236758134308);
+            const double whole = __builtin_rint(quarters);
+            const float t = (float)((quarters - whole) * 1.57079632679489661923), t2 = t * t;
+            const float sn = fmaf(t * t2, fmaf(t2, fmaf(t2, fmaf(t2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), t);
+            const float cs = fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+            const int quadrant = (int)(long)whole & 3;
+            const float x = quadrant & 1 ? sn : cs, y = quadrant & 1 ? cs : sn;
+            c[e] = quadrant == 1 || quadrant == 2 ? -x : x;
+            s[e] = quadrant & 2 ? -y : y;
         }
     }
 }

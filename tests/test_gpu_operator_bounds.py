@@ -156,3 +156,25 @@ def test_decode_and_read_agree_on_the_smallest_scale(ea):  # noqa: F811
     O, tau, _ = ea.entmax_attn_decode_cache4(q.cuda(), cache, i32([[0]]), i32([1]), 2.0, page)
     assert torch.equal(O[0, 0], v[0, 0])                                        # p = 1
     assert tau.item() == np.float32(want[0][0, 0, 0, 3] * 2.0 ** 108 / 8 - 1)
+
+
+# ---- sine and cosine ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_in_fp32_is_known_to_fp32(ea, interleaved):  # noqa: F811
+    """Pairs of (1, 0): the outputs are the cosine and the sine themselves, rounded from 64 bits: half a step, and as much again
+    for a sum of products."""
+    B, N, d = 1, 3000, 128
+    g = torch.Generator().manual_seed(6)
+    x = torch.zeros(B, N, 1, d)
+    x[..., slice(0, d, 2) if interleaved else slice(0, d // 2)] = 1
+    pos = torch.randint(-200000, 200000, (1, B, N), generator=g).to(torch.int32)
+    freq = torch.pow(10000.0, -torch.arange(d // 2, dtype=torch.float64) / (d // 2)).float()
+    y, _ = ea.entmax_attn_qk_norm_rope_fwd(x.cuda(), x.cuda(), pos.cuda(), freq.cuda(), norm=False, interleaved=interleaved)
+    cos, sin = ref.rotation(pos, freq, [d // 2])
+    want = ref.rotate(x.double(), cos, sin, interleaved).transpose(1, 2)
+    err = (y.double().cpu() - want).abs()
+    print("  largest error, in half steps of 1:", err.max().item() / U, flush=True)
+    # relative: the angle's rounding to fp32 u (times the angle, at most pi / 4 for a half that matters), a polynomial's last two
+    # roundings; absolute: the 64-bit angle, 200000 2^-52
+    assert (err <= 3 * U * want.abs() + 2e-10).all(), (err / U).max()
