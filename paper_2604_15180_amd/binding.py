@@ -423,6 +423,8 @@ def entmax_attn_cache_tables(lens, new_lens, block_table, free_pages, free_count
     free_pages [n_pages] and free_count [1] (all int32) are updated in place -> (lens_out [R], token_start [R+1], slots
     [max_tokens], positions [max_tokens], status [4]), int32; `out`: tensors to write them into (lens_out may be lens)."""
     call = "entmax_attn_cache_tables"
+    if out is not None and len(out) != 5:       # (each goes to the library as a pointer of its own)
+        raise ValueError(f"{call}: out must be (lens_out, token_start, slots, positions, status), got {len(out)} tensors")
     dev = _on_gpu(call, lens, new_lens, block_table, free_pages, free_count, *(out or ()))
     if block_table.dim() != 2 or free_pages.dim() != 1:
         raise ValueError(f"{call}: block_table [R,max_blocks], free_pages [n_pages]")

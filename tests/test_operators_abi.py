@@ -138,6 +138,13 @@ def test_bindings_refuse_cpu_tensors_and_wrong_types():
     assert ea.entmax_attn_cache4_empty(3, 2, 64, 16, device="cpu").shape == (3, 2, 16 * 68)
 
 
+@pytest.mark.parametrize("n", [0, 4, 6, 10])
+def test_tables_binding_refuses_outputs_of_another_number(n):
+    i = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="token_start"):
+        ea.entmax_attn_cache_tables(i, i, i[None], i, i, 16, 1, out=(i,) * n)
+
+
 def test_strerror_of_layout(L):
     assert "overlap" in ea.entmax_attn_strerror(LAYOUT)
 
