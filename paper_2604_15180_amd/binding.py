@@ -326,6 +326,12 @@ def _launch(dev, function, *args):
         _check(rc)
 
 
+def _workspace_arg(call, t):
+    """A caller's workspace is taken as all its bytes from its first one on: those of an expanded view are not there."""
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{call}: workspace must be contiguous")
+
+
 def _at(t):
     return None if t is None else t.data_ptr()
 
@@ -396,6 +402,7 @@ def entmax_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_we
     dq, dk like q, k (contiguous, or `out` = (dq, dk) views to write into), weight gradients float32 [d], None for a weight that
     was None."""
     call = "entmax_attn_qk_norm_rope_bwd"
+    _workspace_arg(call, workspace)
     dev = _on_gpu(call, q, k, dq_out, dk_out, positions, inv_freq, q_weight, k_weight, workspace, *(out or ()))
     B, N, Hq, Hk, d, rot, axes, sec = _prep_args(call, q, k, positions, inv_freq, q_weight, k_weight, norm, sections)
     for g, H in ((dq_out, Hq), (dk_out, Hk)):
@@ -516,6 +523,7 @@ def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max
     (O [R,Hq,d], tau [R,Hq], support [R,Hq]).  max_len: the largest length there can be (default: all that the table's pages
     hold); launch and workspace go by it."""
     call = "entmax_attn_decode_cache4"
+    _workspace_arg(call, workspace)
     dev = _on_gpu(call, q, cache, block_table, lens, workspace)
     if q.dim() != 3 or not q.is_contiguous() or block_table.dim() != 2:
         raise ValueError(f"{call}: q contiguous [R,Hq,d], block_table [R,max_blocks]")

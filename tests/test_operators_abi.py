@@ -145,6 +145,15 @@ def test_tables_binding_refuses_outputs_of_another_number(n):
         ea.entmax_attn_cache_tables(i, i, i[None], i, i, 16, 1, out=(i,) * n)
 
 
+def test_bindings_refuse_a_workspace_that_is_a_view_of_less():
+    x, i = torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, dtype=torch.int32)
+    w, f, ws = torch.ones(64), torch.zeros(32), torch.zeros(1, dtype=torch.uint8).expand(1 << 24)
+    with pytest.raises(ValueError, match="workspace"):
+        ea.entmax_attn_qk_norm_rope_bwd(x, x, x, x, i, f, w, w, workspace=ws)
+    with pytest.raises(ValueError, match="workspace"):
+        ea.entmax_attn_decode_cache4(x[0], torch.zeros(1, 1, 16 * 68, dtype=torch.uint8), i, i[0], 1.5, 16, workspace=ws)
+
+
 def test_strerror_of_layout(L):
     assert "overlap" in ea.entmax_attn_strerror(LAYOUT)
 
