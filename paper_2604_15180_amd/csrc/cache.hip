@@ -284,14 +284,6 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
 namespace {
 using namespace ea;
 
-int cache_launched() {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
-    return EA_OK;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 bool cache_shape_ok(int Hk, int d, int page, long n_pages) {
     return Hk > 0 && Hk <= 65535 && (d == 64 || d == 128) && cache_page_ok(page) && n_pages > 0 && n_pages * page <= (long)INT_MAX;
 }
@@ -336,7 +328,7 @@ template <bool WRITE> int rows_run(const RowParams& p, int d, int dtype, hipStre
         else { if (many) rows_launch<WRITE, E, 128, 4>(p, items, s); else rows_launch<WRITE, E, 128, 1>(p, items, s); }
     };
     if (dtype == EA_BF16) pick(Bf16{}); else pick(F32{});
-    return cache_launched();
+    return launched();
 }
 
 }  // namespace
@@ -358,7 +350,7 @@ int entmax_attn_cache_tables(const int32_t* lens, const int32_t* new_lens, int32
     hipLaunchKernelGGL(cache_tables_kernel, dim3(1), dim3(1024), 0, s, p);
     if (max_tokens > TABLE_ROWS_INSIDE) hipLaunchKernelGGL(cache_slots_kernel, dim3((max_tokens + TABLE_SLOTS_THREADS - 1) / TABLE_SLOTS_THREADS),
                                                            dim3(TABLE_SLOTS_THREADS), 0, s, p);
-    return cache_launched();
+    return launched();
 }
 
 size_t entmax_attn_cache4_page_bytes(int Hk, int d, int page_size) {

@@ -597,7 +597,7 @@ int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* b
         (long)n_pages * page_size > (long)INT_MAX || (long)max_blocks * page_size < max_len)
         return EA_ERR_SHAPE;
     if (!isfinite(alpha) || !(alpha > 1.f) || alpha > EA_ALPHA_MAX) return EA_ERR_ALPHA;
-    if (((uintptr_t)q & 15) || ((uintptr_t)cache & 15)) return EA_ERR_LAYOUT;
+    if (!aligned16(q) || !aligned16(cache)) return EA_ERR_LAYOUT;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len))
         return EA_ERR_WORKSPACE;
     Cache4Params p{};
@@ -616,9 +616,7 @@ int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* b
     hipStream_t s = (hipStream_t)hip_stream;
     if (dtype == EA_BF16) { if (d == 64) cache4_run<Bf16, 64>(p, s); else cache4_run<Bf16, 128>(p, s); }
     else { if (d == 64) cache4_run<F32, 64>(p, s); else cache4_run<F32, 128>(p, s); }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
-    return EA_OK;
+    return launched();
 }
 
 }  // extern "C"

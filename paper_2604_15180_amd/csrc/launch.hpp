@@ -13,6 +13,13 @@ constexpr int NBINS = 63;    // histogram bins B per unit (Sec. 3.1): bracket wi
 constexpr int MAX_SWEEPS = 12;
 
 void set_last_hip_error(int e);
+// What a call returns after its launches.
+inline int launched() {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
+    return EA_OK;
+}
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // Records a HIP event on `s` before (which = 0) or after (which = 1) the kernels of timer slot
 // `slot`; does nothing unless timing was switched on for the call in flight.
 void timer_mark(int slot, int which, hipStream_t s);

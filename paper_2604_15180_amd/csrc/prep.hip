@@ -298,8 +298,6 @@ constexpr int BWD_GROUPS = 1024;        // work-groups of the backward: four per
 
 int tokens_per_group(int d) { return 256 / (d / 8); }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 // strides in elements: rows of a tensor start at multiples of 16 bytes
 bool strides_ok(const int64_t* st, int elem_bytes) {
     if (!st) return false;
@@ -373,12 +371,6 @@ dim3 prep_grid(PrepParams& p, int sets, int enough) {
     return dim3(sets, (heads + p.heads_per_group - 1) / p.heads_per_group);
 }
 
-int prep_launched() {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { set_last_hip_error((int)e); return EA_ERR_HIP; }
-    return EA_OK;
-}
-
 template <class E, int D> void fwd_launch(const PrepParams& p, bool neighbours, dim3 grid, hipStream_t s) {
     if (neighbours) hipLaunchKernelGGL((qk_prep_kernel<E, D, true>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((qk_prep_kernel<E, D, false>), grid, dim3(256), 0, s, p);
@@ -410,7 +402,7 @@ int entmax_attn_qk_norm_rope_fwd(const void* q, const void* k, void* q_out, void
     hipStream_t s = (hipStream_t)hip_stream;
     if (dtype == EA_BF16) { if (d == 64) fwd_launch<Bf16, 64>(p, interleaved, grid, s); else fwd_launch<Bf16, 128>(p, interleaved, grid, s); }
     else { if (d == 64) fwd_launch<F32, 64>(p, interleaved, grid, s); else fwd_launch<F32, 128>(p, interleaved, grid, s); }
-    return prep_launched();
+    return launched();
 }
 
 size_t entmax_attn_qk_norm_rope_workspace_bytes(int d) {
@@ -450,7 +442,7 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
     else { if (d == 64) bwd_launch<F32, 64>(p, interleaved, grid, s); else bwd_launch<F32, 128>(p, interleaved, grid, s); }
     if (want_dw)
         hipLaunchKernelGGL(qk_prep_dw_kernel, dim3(2 * d / 16), dim3(1024), 0, s, p.part, dq_weight, dk_weight, groups, d);
-    return prep_launched();
+    return launched();
 }
 
 }  // extern "C"
