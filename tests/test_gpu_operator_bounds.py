@@ -178,3 +178,15 @@ def test_rotation_in_fp32_is_known_to_fp32(ea, interleaved):  # noqa: F811
     # relative: the angle's rounding to fp32 u (times the angle, at most pi / 4 for a half that matters), a polynomial's last two
     # roundings; absolute: the 64-bit angle, 200000 2^-52
     assert (err <= 3 * U * want.abs() + 2e-10).all(), (err / U).max()
+
+
+# ---- rows whose squares pass the largest float --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_rows_whose_squares_overflow(ea, dtype):  # noqa: F811
+    """Sums of squares from 2^128 on: zeros.  64 elements of 2^61 are the first, of 2^60 still normed."""
+    x = torch.ones(1, 1, 2, 64)
+    x[0, 0, 0], x[0, 0, 1] = 2.0 ** 61, 2.0 ** 60
+    x = x.to(DT[dtype]).cuda()
+    y, _ = ea.entmax_attn_qk_norm_rope_fwd(x, x, None, None)
+    assert (y[0, 0] == 0).all() and (y[0, 1] == 1).all()
