@@ -230,8 +230,9 @@ int entmax_attn_decode_static(const void* q, const void* K, const void* V,
                               int B, int H, int N, int d, int dtype, float alpha, void* hip_stream);
 
 /*
- * Queries and keys as entmax_attn_fwd takes them, from what a layer's projections give: the RMS norm
- * of each head's row and its rotation by the token's position, in one pass.
+ * Queries and keys in the attention's layout, from what a layer's projections give: the RMS norm
+ * of each head's row and its rotation by the token's position, in one pass.  With Hq = Hk and N a multiple of 64 they are what
+ * entmax_attn_fwd takes; with other N and fewer key heads than query heads, what the 4-bit cache and the decode from it take (below).
  *     y = w x / sqrt(mean(x^2) + eps)                               (norm != 0; else y = x)
  *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = position[axis(i)] * inv_freq[i]
  * for the pairs i = 0 .. rot/2 - 1 of the row's first `rot` elements: (i, i + rot/2), or the neighbours
@@ -245,11 +246,12 @@ int entmax_attn_decode_static(const void* q, const void* K, const void* V,
  *   q_weight, k_weight in [d] float32, may be NULL (ones); they go with norm != 0
  *   positions   in   [n_axes,B,N] int32, any value;  inv_freq in [rot/2] float32 (both unused if rot = 0)
  *   sections    in   HOST pointer to n_axes pair counts that sum to rot/2; may be NULL for one axis
- * Angles are formed in 64 bits from the int32 position and the float32 frequency; everything else is in float32,
- * rounded once to `dtype`.  B N <= 2^27, d 64 or 128, rot a multiple of 8 (0 .. d), at most 4 axes, eps > 0.
+ * Angles are formed in 64 bits from the int32 position and the float32 frequency; everything else is in float32
+ * (a row whose squares add up to 2^128 or more is normed to zeros), rounded once to `dtype`.  B N <= 2^27, d 64 or 128, rot a multiple of 8 (0 .. d), at most 4 axes, eps > 0.
  * EA_ERR_LAYOUT if q, k, an output, a weight or a stride is not a multiple of 16 bytes.
  *
- * entmax_attn_qk_norm_rope_bwd: the gradient.  It takes dQ, dK as entmax_attn_bwd returns them.
+ * entmax_attn_qk_norm_rope_bwd: the gradient.  It takes dQ, dK as entmax_attn_bwd returns them, where the shape is one of
+ * entmax_attn_fwd's; from any other attention, dQ and dK summed over the query heads that share a key head.
  *   dq_out, dk_out in [B,Hq,N,d], [B,Hk,N,d] float32, contiguous
  *   dq, dk      out  like q, k, of `dtype`, with strides of their own (rows must not overlap); for an input whose rows
  *                    repeat (stride 0) they hold the gradient of each use
@@ -321,6 +323,7 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  *   O           out  [R,Hq,d] float32;  tau out [R,Hq] float32, raw convention as in entmax_attn_fwd
  *   support     out  [R,Hq] int32, may be NULL: number of keys with p > 0
  *   max_len          at least the largest length, at most 2^22 and max_blocks * page_size: the launch and the workspace go by it
+ *                    (about 4 R Hq max_len bytes, whatever the lengths: 1.1 GB for 64 requests of 32 heads with max_len 131072)
  * A request of length 0 gets O = 0, tau = 0, support 0.  One whose length is negative or above max_len, or that has a
  * page id outside 0 .. n_pages - 1 among the pages it attends to, gets NaN and support -1, and so does a head whose query or
  * keys hold an infinity or a NaN, or where 2^floor(log2 max|q|) of the head's query times the scale of a block of its keys

@@ -521,7 +521,8 @@ def entmax_attn_decode_cache4_workspace_bytes(R, Hq, Hk, d, max_len):
 def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max_len=None, workspace=None):
     """One query per head and request against a 4-bit cache: q [R,Hq,d], block_table [R,max_blocks], lens [R] (int32) ->
     (O [R,Hq,d], tau [R,Hq], support [R,Hq]).  max_len: the largest length there can be (default: all that the table's pages
-    hold); launch and workspace go by it."""
+    hold); launch and workspace go by it.  workspace: entmax_attn_decode_cache4_workspace_bytes bytes, about 4 R Hq max_len; without it
+    they are allocated in every call."""
     call = "entmax_attn_decode_cache4"
     _workspace_arg(call, workspace)
     dev = _on_gpu(call, q, cache, block_table, lens, workspace)

@@ -151,7 +151,7 @@ EA_DEV float c4_from_ordered(unsigned int u) { return __uint_as_float((u & 0x800
 // (contraction indices 0 .. 63 of the operand) one, the upper half the other.  Then (PAIR) up to eight query heads stand in columns 0 .. 7
 // with their terms in the lower indices, for the first set, and once more in columns 8 .. 15 in the upper ones, for the second,
 // with zeros elsewhere: both sets in one instruction per term.  More heads have their terms in both halves, and the keys are worked on
-// one set at a time, with zeros in place of the other's (32 heads x 131072 keys, one head a key head: 34 us, PAIR 30; fp32 queries 41 and 32).
+// one set at a time, with zeros in place of the other's (32 heads x 131072 keys, one head a key head: 38 us, PAIR 32; fp32 queries 40 and 32).
 // Result: lane (n, g) holds column n's scores with keys 4 g .. 4 g + 3 of a set.  A wave keeps two blocks of 64 keys on their way: as soon as
 // the matrix cores have taken a tile, the same tile of the block after the next is requested.  The addresses of all its keys are
 // formed at once, a lane for each sixteen.
@@ -299,9 +299,8 @@ __global__ __launch_bounds__(64 * C4_WAVES) void cache4_scores_kernel(Cache4Para
 
 // A wave takes a part of the head's blocks, in order, and keeps its candidates to itself: the waves meet only in the sums of an
 // evaluation and of the output.  SPLIT work-groups do the same for a head, each for a part of the output's elements: with few heads the
-// card is empty, and what one CU can have on its way limits how fast the rows of a long support are read (32 heads of 131072 keys at
-// alpha 1.05: 1726 us with one, 566 with four; flat heads at alpha 1.5: 203 and 149; short supports the same; 256 heads of 1000 keys
-// 7.2 and 12.9).
+// card is empty, and what one CU can have on its way limits how fast the rows of a long support are read (32 heads of 131072 keys, 8 key heads, at
+// alpha 1.05: 1620 us with one, 522 with four; flat heads at alpha 1.5: 203 and 149; short supports the same; the choice: cache4_run).
 template <int D, int AM, int NW, int SPLIT>
 __global__ __launch_bounds__(64 * NW) void cache4_entmax_kernel(Cache4Params p) {
     constexpr int SEG = 512, ROW = D / 2, SROW = D / 32, DS = D / SPLIT, LPR = DS / 8, AT_ONCE = 64 / LPR, U = 4;
@@ -548,6 +547,12 @@ void cache4_run(const Cache4Params& p, hipStream_t s) {
     const dim3 grid(p.Hk * p.colgroups, p.R, (p.max_len + per_group - 1) / per_group), block(64 * C4_WAVES);
     if (D == 64 && p.G <= 8) hipLaunchKernelGGL((cache4_scores_kernel<E, D, D == 64>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((cache4_scores_kernel<E, D, false>), grid, block, 0, s, p);
+    // Four work-groups per head up to 64 heads, one from 65 on; there eight waves below 512 heads, four from 512 on.  Both sides of the
+    // borders, D = 128, us (alpha 1.5 with short supports at 1000 / 32768 keys; alpha 1.05 with supports of most keys, the same):
+    //   64 heads: four work-groups 8.0 / 8.1, 10.3 / 146, one 7.6 / 8.0, 14.4 / 416;  96: four 9.3 / 9.0, 12.7 / 182, one 7.6 / 8.0, 14.7 / 417
+    //   384 heads: eight waves 9.4 / 10.9, 23 / 556, four 7.6 / 12.6, 30 / 915;  512: eight 9.3 / 11.8, 24 / 599, four 7.8 / 14.0, 33 / 984;
+    //   768: eight 11.2 / 13.5, 29 / 693, four 8.6 / 13.5, 36 / 1085
+    // The host knows neither the lengths nor the supports: the borders lie where short supports, the rule, begin to lose.
     const long heads = (long)p.R * p.Hq;
     if (heads <= 64) cache4_entmax<D, 8, 4>(p, s);
     else if (heads < 512) cache4_entmax<D, 8, 1>(p, s);
@@ -563,8 +568,8 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Keys per wave of the score kernel: few enough that the waves of all heads number about 4096 (sixteen per CU), where several requests are
 // taken to be half as long as the longest, at least C4_BLOCK, and at most C4_MAX_PART: the longest request's keys are not to queue up
-// behind few waves.  (24 requests up to 8192 keys, 8 key heads: 192 or 256 keys 12 us, 512 keys 15; 48 requests up to 32768: 256
-// keys 40 us, 512 41, 1024 46; one of 131072, 32 key heads: 54, 51, 50.)
+// behind few waves.  (24 requests up to 8192 keys, 8 key heads: 192 keys 10 us, 256 11, 512 12.5; 48 requests up to 32768: 41 to 42 us
+// from 192 to 512; one of 131072, 32 key heads: 192 and 256 keys 55 us, 512 51.)
 int cache4_part(int R, int Hq, int Hk, int max_len) {
     const long groups = (long)R * Hk * ((Hq / Hk + 15) / 16);
     const long part = ((long)max_len * groups / (R > 1 ? 8192 : 4096) + 63) / 64 * 64;
