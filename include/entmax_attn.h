@@ -349,6 +349,92 @@ int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* b
                               int R, int Hq, int Hk, int d, int dtype, int max_len, int max_blocks, int n_pages, int page_size,
                               float alpha, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * The same in 8 bits, for keys and values that 4 bits do not hold well enough: about twice the bytes.
+ *
+ * Format.  `cache` is [n_pages][entmax_attn_cache8_page_bytes(Hk, d, page_size)] bytes, 16-byte aligned.  Head h's part of a page starts at
+ * h times 2 page_size d + max(16, page_size / 2) bytes and is
+ *     key codes [page_size][d], value codes [page_size][d], key scales [page_size/16], value scales [page_size/16] (float32).
+ * The d values of 16 neighbouring tokens share a scale; a value is its code (a signed byte, -127 .. 127) times the scale's
+ * magnitude.  Code -128 is not a number, and a scale whose sign bit is clear has none in its block.  Tables and slots as above.
+ *
+ * entmax_attn_cache8_write: keys and values of T tokens to their slots, arguments as entmax_attn_cache4_write.  Rows of one block
+ * have to stand next to each other in the call, as the rows of a request do that entmax_attn_cache_tables makes slots for; they are
+ * appended: with s_new = max|x| / 127 over them and one head (rounded to float32, at least 2^-126 unless they are all zero; infinities and NaN
+ * left out), the block's scale becomes the larger of s_new and what it was.  If it grows, the codes c of the rows in front of the
+ * lowest one written become c s_old / s rounded to the nearest integer (ties to the even one, here and below).  If row 0 of the block is
+ * written, the block starts anew with s_new.  A code is x / s rounded to the nearest integer, an infinity or a NaN code -128.  What rows
+ * behind the lowest one written held, and are not written themselves, is lost.  Where the slots of a call are not different, or rows of one block
+ * stand apart, the codes and scales of that block are undefined.
+ *
+ * entmax_attn_cache8_read: as entmax_attn_cache4_read; a value is code times scale in float32, rounded to `dtype`.
+ *
+ * entmax_attn_decode_cache8: as entmax_attn_decode_cache4, against this cache, and with a sliding window:
+ *   window, sinks    with window > 0 the query of a request of length n sees the keys j with j >= n - window and those with j < sinks; with
+ *                    window = 0 all.  Pages without a key that is seen are not read, nor are their entries of block_table.
+ * The workspace is about 4 R Hq min(max_len, window + sinks) bytes.  A head gets NaN and support -1 where its query, or a key that it sees, holds an
+ * infinity or a NaN, where a page id that it needs is out of range, or where 2^floor(log2 max|q|) of its query times the scale of
+ * sixteen keys that it sees reaches 2^104.  Scores: integer products of the codes with q in three (bf16) or four (float32) 8-bit terms, summed
+ * exactly; q is known to 2^-21 (bf16; exact down to 2^-13) or 2^-28 (float32) of the power of two at or below the largest of its row (rows
+ * below 2^-90 lose more).  All else as there.
+ */
+size_t entmax_attn_cache8_page_bytes(int Hk, int d, int page_size);      /* 0 for a bad shape */
+int entmax_attn_cache8_write(const void* K, const void* V, const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                             void* cache, int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream);
+int entmax_attn_cache8_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
+                            int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream);
+size_t entmax_attn_decode_cache8_workspace_bytes(int R, int Hq, int Hk, int d, int max_len, int window, int sinks);   /* 0 for a bad shape */
+int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* block_table, const int32_t* lens,
+                              float* O, float* tau, int32_t* support,
+                              int R, int Hq, int Hk, int d, int dtype, int max_len, int max_blocks, int n_pages, int page_size,
+                              int window, int sinks, float alpha, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Pages that several requests hold, in either cache: several answers to one prompt, beams, a prefix that many requests begin with.
+ *   shares      in/out [n_pages] int32: holders of a page beyond the first, 0 at the start.  entmax_attn_cache_tables knows nothing of
+ *               them: it may grow any request, but a request whose pages others hold is shortened and ended by entmax_attn_cache_fork.
+ *
+ * entmax_attn_cache_fork: request r becomes the first new_lens[r] tokens of what request parents[r] held before the call, all
+ * requests at once: itself shortened (parents[r] = r), ended (0), left as it is (its own length), or a fork of another.
+ *   lens, parents, new_lens in [R] int32; a request with a parent that is none, a new length that is negative or above its parent's, or a length of its own
+ *               that is negative or above max_blocks * page_size stays as it is
+ *   block_table, free_pages, free_count in/out as in entmax_attn_cache_tables.  First the pages that nobody holds any more go on top of the
+ *               stack, the last request's last page first (a page that several requests leave counts as the last one's).  Then each
+ *               request that ends inside a page that others hold too gets a page of its own from the top, in order; one of those that end in a page
+ *               keeps it, if none holds it whole: the first that is its own parent, else the first.  (New tokens may then be
+ *               written to every request.)
+ *   lens_out    out    [R] int32: the lengths now; may be `lens` itself, not parents or new_lens.  Where no page is left for a copy, the request
+ *               ends before the page that was to be copied
+ *   moves       out    [R][2] int32, 8-byte aligned: pages to be copied, from and to, before either is written to; -1 behind the last
+ *   status      out    [4] int32: moves, requests for whose copy no page was left, requests that stay as they are because of
+ *               their arguments, page ids outside 0 .. n_pages - 1 met
+ *   workspace   entmax_attn_cache_fork_workspace_bytes bytes, 256-byte aligned
+ *
+ * entmax_attn_cache_compact: the pages in use move to the front: with `used` pages not on the stack, the i-th free page below `used` takes the
+ * i-th page in use from `used` on.  Every output may be its input itself.
+ *   table_out   out    [R][max_blocks]: block_table with the pages' new ids, all other entries as they were
+ *   free_out    out    [n_pages]: the stack of the free pages, the lowest on top; entries behind it as they were
+ *   shares_out  out    [n_pages] (0 for a free page); NULL if shares is
+ *   moves       out    [n_pages / 2][2] int32, 8-byte aligned: from and to, -1 behind the last; no page that is moved from is moved to
+ *   status      out    [4] int32: moves, pages in use, lengths out of range (their tables stay), page ids that are out of range, twice on the
+ *               stack, or free but in a table (such entries stay)
+ *
+ * entmax_attn_cache_copy: pages moves[i] = (from, to), i < count[0] and i < max_moves, of page_bytes (a multiple of 16) bytes each, from `src` to `dst`, which may
+ * be one cache if no page is both, nor the target of two.  Pairs with an id out of range are skipped.
+ *
+ * Results of all three repeat bit for bit.  R <= 4096, max_blocks * page_size <= 2^22, n_pages * page_size < 2^31.
+ */
+size_t entmax_attn_cache_fork_workspace_bytes(int R, int max_blocks);    /* 0 for a bad shape */
+int entmax_attn_cache_fork(const int32_t* lens, const int32_t* parents, const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
+                           int32_t* free_count, int32_t* shares, int32_t* lens_out, int32_t* moves, int32_t* status,
+                           int R, int max_blocks, int page_size, int n_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t entmax_attn_cache_compact_workspace_bytes(int n_pages);           /* 0 for a bad number */
+int entmax_attn_cache_compact(const int32_t* lens, const int32_t* block_table, const int32_t* free_pages, const int32_t* free_count,
+                              const int32_t* shares, int32_t* table_out, int32_t* free_out, int32_t* shares_out, int32_t* moves, int32_t* status,
+                              int R, int max_blocks, int page_size, int n_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+int entmax_attn_cache_copy(const void* src, void* dst, const int32_t* moves, const int32_t* count, int max_moves, size_t page_bytes,
+                           int src_pages, int dst_pages, void* hip_stream);
+
 /* Static, human-readable text for a return code. */
 const char* entmax_attn_strerror(int code);
 

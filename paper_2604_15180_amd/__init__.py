@@ -11,4 +11,7 @@ from .binding import (  # noqa: F401
     entmax_attn_qk_norm_rope_fwd, entmax_attn_qk_norm_rope_bwd, entmax_attn_qk_norm_rope_workspace_bytes,
     entmax_attn_cache_tables, entmax_attn_cache4_empty, entmax_attn_cache4_page_bytes, entmax_attn_cache4_write,
     entmax_attn_cache4_read, entmax_attn_decode_cache4, entmax_attn_decode_cache4_workspace_bytes,
+    entmax_attn_cache8_empty, entmax_attn_cache8_page_bytes, entmax_attn_cache8_write, entmax_attn_cache8_read,
+    entmax_attn_decode_cache8, entmax_attn_decode_cache8_workspace_bytes, entmax_attn_cache_fork, entmax_attn_cache_fork_workspace_bytes,
+    entmax_attn_cache_compact, entmax_attn_cache_compact_workspace_bytes, entmax_attn_cache_copy,
 )

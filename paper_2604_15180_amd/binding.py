@@ -101,6 +101,26 @@ def lib():
         L.entmax_attn_decode_cache4_workspace_bytes.argtypes = [ci] * 5
         L.entmax_attn_decode_cache4.restype = ci
         L.entmax_attn_decode_cache4.argtypes = [vp] * 7 + [ci] * 9 + [cf, vp, sz, vp]
+        L.entmax_attn_cache8_page_bytes.restype = sz
+        L.entmax_attn_cache8_page_bytes.argtypes = [ci, ci, ci]
+        L.entmax_attn_cache8_write.restype = ci
+        L.entmax_attn_cache8_write.argtypes = [vp] * 6 + [ci] * 6 + [vp]
+        L.entmax_attn_cache8_read.restype = ci
+        L.entmax_attn_cache8_read.argtypes = [vp] * 6 + [ci] * 6 + [vp]
+        L.entmax_attn_decode_cache8_workspace_bytes.restype = sz
+        L.entmax_attn_decode_cache8_workspace_bytes.argtypes = [ci] * 7
+        L.entmax_attn_decode_cache8.restype = ci
+        L.entmax_attn_decode_cache8.argtypes = [vp] * 7 + [ci] * 11 + [cf, vp, sz, vp]
+        L.entmax_attn_cache_fork_workspace_bytes.restype = sz
+        L.entmax_attn_cache_fork_workspace_bytes.argtypes = [ci] * 2
+        L.entmax_attn_cache_fork.restype = ci
+        L.entmax_attn_cache_fork.argtypes = [vp] * 10 + [ci] * 4 + [vp, sz, vp]
+        L.entmax_attn_cache_compact_workspace_bytes.restype = sz
+        L.entmax_attn_cache_compact_workspace_bytes.argtypes = [ci]
+        L.entmax_attn_cache_compact.restype = ci
+        L.entmax_attn_cache_compact.argtypes = [vp] * 10 + [ci] * 4 + [vp, sz, vp]
+        L.entmax_attn_cache_copy.restype = ci
+        L.entmax_attn_cache_copy.argtypes = [vp] * 4 + [ci, sz, ci, ci, vp]
         L.entmax_attn_strerror.restype = ctypes.c_char_p
         L.entmax_attn_strerror.argtypes = [ci]
         _lib = L
@@ -541,6 +561,179 @@ def entmax_attn_decode_cache4(q, cache, block_table, lens, alpha, page_size, max
             tau.data_ptr(), support.data_ptr(), R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, float(alpha),
             ws.data_ptr(), ws.numel() * ws.element_size())
     return O, tau, support
+
+
+# ---- the 8-bit cache, and pages that requests share ---------------------------------------------
+
+_INT_MAX = (1 << 31) - 1
+
+
+def entmax_attn_cache8_page_bytes(Hk, d, page_size):
+    return int(lib().entmax_attn_cache8_page_bytes(Hk, d, page_size))
+
+
+def entmax_attn_cache8_empty(n_pages, Hk, d, page_size, device="cuda"):
+    """A cache of n_pages pages: uint8 [n_pages, Hk, 2 page_size d + max(16, page_size / 2)], all values zero."""
+    nbytes = entmax_attn_cache8_page_bytes(Hk, d, page_size)
+    if nbytes == 0 or n_pages <= 0:
+        raise ValueError("entmax_attn_cache8_empty: Hk, n_pages > 0, d 64 or 128, page_size 16, 32, 64, 128 or 256")
+    return torch.zeros((n_pages, Hk, nbytes // Hk), dtype=torch.uint8, device=device)
+
+
+def _cache8_args(call, cache, d, page_size):
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.shape[2] != 2 * page_size * d + max(16, page_size // 2):
+        raise ValueError(f"{call}: cache must be contiguous uint8 [n_pages, Hk, 2 page_size d + max(16, page_size / 2)]")
+    return cache.shape[0], cache.shape[1]
+
+
+def entmax_attn_cache8_write(K, V, slots, cache, page_size):
+    """K, V [T,Hk,d] (any strides between rows) appended at the slots [T] (int32; negative: skipped) of an 8-bit cache; rows of
+    one block of 16 slots stand next to each other, as entmax_attn_cache_tables gives them."""
+    call = "entmax_attn_cache8_write"
+    dev = _on_gpu(call, K, V, slots, cache)
+    d = K.shape[-1]
+    pages, Hk = _cache8_args(call, cache, d, page_size)
+    ks, vs = _cache_rows(call, K, V, slots, Hk)
+    _launch(dev, lib().entmax_attn_cache8_write, K.data_ptr(), V.data_ptr(), ks, vs, slots.data_ptr(), cache.data_ptr(), K.shape[0], Hk, d,
+            _dtype_code(K.dtype), pages, page_size)
+
+
+def entmax_attn_cache8_read(cache, slots, page_size, d, dtype=torch.bfloat16, out=None):
+    """The rows of the slots [T] as the cache holds them -> (K, V) [T,Hk,d]; `out` = (K, V) to write into (any strides between
+    rows; rows of negative slots are left as they were, and are undefined without `out`)."""
+    call = "entmax_attn_cache8_read"
+    dev = _on_gpu(call, cache, slots, *(out or ()))
+    pages, Hk = _cache8_args(call, cache, d, page_size)
+    if out is None:
+        out = (cache.new_empty((slots.numel(), Hk, d), dtype=dtype), cache.new_empty((slots.numel(), Hk, d), dtype=dtype))
+    K, V = out
+    if K.shape[-1] != d:
+        raise ValueError(f"{call}: out must be [T,Hk,{d}]")
+    ks, vs = _cache_rows(call, K, V, slots, Hk)
+    _launch(dev, lib().entmax_attn_cache8_read, cache.data_ptr(), slots.data_ptr(), K.data_ptr(), V.data_ptr(), ks, vs, K.shape[0], Hk, d,
+            _dtype_code(K.dtype), pages, page_size)
+    return K, V
+
+
+def entmax_attn_decode_cache8_workspace_bytes(R, Hq, Hk, d, max_len, window=0, sinks=0):
+    return int(lib().entmax_attn_decode_cache8_workspace_bytes(R, Hq, Hk, d, max_len, min(window, _INT_MAX), min(sinks, _INT_MAX)))
+
+
+def entmax_attn_decode_cache8(q, cache, block_table, lens, alpha, page_size, max_len=None, window=0, sinks=0, workspace=None):
+    """entmax_attn_decode_cache4 against an 8-bit cache -> (O [R,Hq,d], tau [R,Hq], support [R,Hq]).  window > 0: a query sees
+    the last `window` tokens of its request and the first `sinks`.  workspace: entmax_attn_decode_cache8_workspace_bytes bytes, about
+    4 R Hq min(max_len, window + sinks); without it they are allocated in every call."""
+    call = "entmax_attn_decode_cache8"
+    _workspace_arg(call, workspace)
+    dev = _on_gpu(call, q, cache, block_table, lens, workspace)
+    if q.dim() != 3 or not q.is_contiguous() or block_table.dim() != 2:
+        raise ValueError(f"{call}: q contiguous [R,Hq,d], block_table [R,max_blocks]")
+    R, Hq, d = q.shape
+    window, sinks = min(window, _INT_MAX), min(sinks, _INT_MAX)         # (no request is longer)
+    pages, Hk = _cache8_args(call, cache, d, page_size)
+    _int32(call, "block_table", block_table, (R, block_table.shape[1]))
+    _int32(call, "lens", lens, (R,))
+    blocks = block_table.shape[1]
+    if max_len is None:
+        max_len = blocks * page_size
+    O, tau, support = q.new_empty((R, Hq, d), dtype=torch.float32), q.new_empty((R, Hq), dtype=torch.float32), lens.new_empty((R, Hq))
+    ws = workspace
+    if ws is None:
+        ws = _workspace(entmax_attn_decode_cache8_workspace_bytes(R, Hq, Hk, d, max_len, window, sinks), q.device)
+    _launch(dev, lib().entmax_attn_decode_cache8, q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), lens.data_ptr(), O.data_ptr(),
+            tau.data_ptr(), support.data_ptr(), R, Hq, Hk, d, _dtype_code(q.dtype), max_len, blocks, pages, page_size, window, sinks,
+            float(alpha), ws.data_ptr(), ws.numel() * ws.element_size())
+    return O, tau, support
+
+
+def _tables_args(call, lens, block_table, free_pages, free_count, shares):
+    if block_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError(f"{call}: block_table [R,max_blocks], free_pages [n_pages]")
+    R, blocks = block_table.shape
+    _int32(call, "lens", lens, (R,))
+    _int32(call, "block_table", block_table, (R, blocks))
+    _int32(call, "free_pages", free_pages, free_pages.shape)
+    _int32(call, "free_count", free_count, (1,))
+    if shares is not None:
+        _int32(call, "shares", shares, free_pages.shape)
+    return R, blocks, free_pages.numel()
+
+
+def entmax_attn_cache_fork_workspace_bytes(R, max_blocks):
+    return int(lib().entmax_attn_cache_fork_workspace_bytes(R, max_blocks))
+
+
+def entmax_attn_cache_fork(lens, parents, new_lens, block_table, free_pages, free_count, shares, page_size, out=None, workspace=None):
+    """Request r becomes the first new_lens[r] tokens of what request parents[r] held, all at once (parents[r] = r: shortened, ended or left
+    as it is).  block_table [R,max_blocks], free_pages [n_pages], free_count [1] and shares [n_pages] (holders of a page beyond the
+    first; all int32) are updated in place -> (lens_out [R], moves [R,2], status [4]), int32: moves[:status[0]] are the pages to be
+    copied with entmax_attn_cache_copy(cache, moves, status[:1]).  `out`: tensors to write them into (lens_out may be lens)."""
+    call = "entmax_attn_cache_fork"
+    _workspace_arg(call, workspace)
+    if out is not None and len(out) != 3:
+        raise ValueError(f"{call}: out must be (lens_out, moves, status), got {len(out)} tensors")
+    dev = _on_gpu(call, lens, parents, new_lens, block_table, free_pages, free_count, shares, workspace, *(out or ()))
+    R, blocks, pages = _tables_args(call, lens, block_table, free_pages, free_count, shares)
+    _int32(call, "parents", parents, (R,))
+    _int32(call, "new_lens", new_lens, (R,))
+    if out is None:
+        moves, lens_out, status = torch.empty(3 * R + 4, dtype=torch.int32, device=lens.device).split_with_sizes([2 * R, R, 4])
+        out = lens_out, moves.view(R, 2), status
+    else:
+        for name, t, shape in zip(("lens_out", "moves", "status"), out, ((R,), (R, 2), (4,))):
+            _int32(call, name, t, shape)
+    ws = workspace if workspace is not None else _workspace(entmax_attn_cache_fork_workspace_bytes(R, blocks), lens.device)
+    _launch(dev, lib().entmax_attn_cache_fork, lens.data_ptr(), parents.data_ptr(), new_lens.data_ptr(), block_table.data_ptr(),
+            free_pages.data_ptr(), free_count.data_ptr(), shares.data_ptr(), *[t.data_ptr() for t in out], R, blocks, page_size, pages,
+            ws.data_ptr(), ws.numel() * ws.element_size())
+    return out
+
+
+def entmax_attn_cache_compact_workspace_bytes(n_pages):
+    return int(lib().entmax_attn_cache_compact_workspace_bytes(n_pages))
+
+
+def entmax_attn_cache_compact(lens, block_table, free_pages, free_count, shares, page_size, out=None, workspace=None):
+    """The pages in use move to the front of a cache -> (block_table, free_pages, shares, moves [n_pages / 2, 2], status [4]), int32:
+    the tables, the stack and the holders (None if shares is None) afterwards, and in moves[:status[0]] the pages to be copied with
+    entmax_attn_cache_copy(cache, moves, status[:1]).  `out`: tensors to write them into; the first three may be the inputs."""
+    call = "entmax_attn_cache_compact"
+    _workspace_arg(call, workspace)
+    if out is not None and len(out) != 5:
+        raise ValueError(f"{call}: out must be (block_table, free_pages, shares, moves, status), got {len(out)} tensors")
+    dev = _on_gpu(call, lens, block_table, free_pages, free_count, shares, workspace, *(out or ()))
+    R, blocks, pages = _tables_args(call, lens, block_table, free_pages, free_count, shares)
+    if out is None:
+        out = (torch.empty_like(block_table), torch.empty_like(free_pages), None if shares is None else torch.empty_like(shares),
+               lens.new_empty((pages // 2, 2)), lens.new_empty(4))
+    else:
+        if (out[2] is None) != (shares is None):
+            raise ValueError(f"{call}: shares and its output go together")
+        for name, t, shape in zip(("block_table", "free_pages", "shares", "moves", "status"), out,
+                                  ((R, blocks), (pages,), (pages,), (pages // 2, 2), (4,))):
+            if t is not None:
+                _int32(call, name, t, shape)
+    ws = workspace if workspace is not None else _workspace(entmax_attn_cache_compact_workspace_bytes(pages), lens.device)
+    _launch(dev, lib().entmax_attn_cache_compact, lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+            _at(shares), *[_at(t) for t in out], R, blocks, page_size, pages, ws.data_ptr(), ws.numel() * ws.element_size())
+    return tuple(out)
+
+
+def entmax_attn_cache_copy(cache, moves, count, dst=None):
+    """Pages moves[i] = (from, to) [n,2] int32, the first count[0] of them, from `cache` to `dst` (default: within it): 4-bit or 8-bit
+    caches [n_pages, Hk, bytes] of one shape but for their number of pages."""
+    call = "entmax_attn_cache_copy"
+    to = cache if dst is None else dst
+    dev = _on_gpu(call, cache, moves, count, dst)
+    for t in (cache, to):
+        if t.dtype != torch.uint8 or t.dim() != 3 or not t.is_contiguous():
+            raise ValueError(f"{call}: a cache must be contiguous uint8 [n_pages, Hk, bytes]")
+    if cache.shape[1:] != to.shape[1:]:
+        raise ValueError(f"{call}: pages of {list(cache.shape[1:])} and {list(to.shape[1:])} bytes")
+    _int32(call, "moves", moves, (moves.shape[0], 2))
+    _int32(call, "count", count, (1,))
+    _launch(dev, lib().entmax_attn_cache_copy, cache.data_ptr(), to.data_ptr(), moves.data_ptr(), count.data_ptr(), moves.shape[0],
+            cache.shape[1] * cache.shape[2], cache.shape[0], to.shape[0])
 
 
 def entmax_attn_mfma_probe(data, sink, groups, iters):

@@ -1,9 +1,10 @@
-// The paged 4-bit cache of a serving program: block tables and slots made on the GPU, rows written to their slots and
-// read back (layout: cache4.hpp).
+// The paged caches of a serving program: block tables and slots made on the GPU, rows written to their slots and
+// read back (layouts: cache4.hpp, cache8.hpp).
 #include <limits.h>
 #include <math.h>
 
 #include "cache4.hpp"
+#include "cache8.hpp"
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -34,18 +35,6 @@ struct TableParams {
     int32_t* status;           // [4]
     int R, blocks, page_shift, n_pages, rows;
 };
-
-EA_DEV int pages_of(int len, int shift) { return (len + (1 << shift) - 1) >> shift; }
-
-// largest r with pref[r] <= i, for i < pref[R] (so that request r has an item i)
-EA_DEV int owner(const int32_t* pref, int R, int i) {
-    int lo = 0, hi = R;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (pref[mid] <= i) lo = mid; else hi = mid;
-    }
-    return lo;
-}
 
 // position and slot of token row t of request r (the table is final)
 EA_DEV void table_row(const TableParams& p, int t, int r, int start, int end, bool granted) {
@@ -279,6 +268,148 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
     }
 }
 
+// ---- rows in 8 bits -------------------------------------------------------------------------------------------------
+// A block is 16 tokens of a head's keys or values with one scale s = max|x| / 127, rounded to float32; a code is the integer nearest to
+// x / s, ties to the even one.  Rows are appended: those of a call that stand next to each other and go to one block are one run, which a wave
+// takes as a whole for one head's keys or values.  The rows in front of a run's first keep their codes, unless the run's own scale is
+// larger than the block's: then it becomes the block's, and they are rounded once more.  A run that begins with row 0
+// begins its block.
+// The nearest integer n is that of x times 1 / s, which is off by up to 2^-16; the remainder x - n s, exact in one fused
+// multiply-add, then tells whether n is the one (halves are exact, too).  Kept codes are rounded in 64 bits, where c s_old is exact.
+
+constexpr int C8_FEW = 1 << 15;         // waves up to which a wave looks after one token's run
+
+// The integer in -127 .. 127 nearest to x / s, ties to even; |x| <= 127 s (1 + 2^-24), inv = 1 / s
+EA_DEV int nearest_code(float x, float s, float inv) {
+    float n = rintf(x * inv);
+    const float rest = fmaf(-n, s, x), twice = 2.f * fabsf(rest);
+    if (twice > s || (twice == s && ((int)n & 1))) n += copysignf(1.f, rest);
+    return (int)fminf(fmaxf(n, -127.f), 127.f);
+}
+
+template <class E, int D, int ROWS>
+__global__ __launch_bounds__(256) void cache8_write_kernel(RowParams p, unsigned int waves) {
+    using elem = typename E::elem;
+    typedef elem vec __attribute__((ext_vector_type(8)));
+    constexpr int LPR = D / 8, AT_ONCE = 64 / LPR, STEPS = C8_BLOCK / AT_ONCE;
+    const unsigned int id = blockIdx.x * 4u + (unsigned int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = 2u * p.Hk;
+    if (id >= waves) return;
+    const int lane = threadIdx.x & 63, sub = lane % LPR, rsel = lane / LPR;
+    const int t0 = (int)(id / per) * ROWS, which = id % per >= (unsigned int)p.Hk, h = (int)(id % per) - (which ? p.Hk : 0);
+    // lane k: the row before t0 + k and this one.  Runs begin where the block changes (or the call does).
+    const int shift = p.page_shift, t = t0 + lane;
+    auto block_of = [&](int row) {
+        const int slot = row >= 0 && row < p.T ? p.slots[row] : -1;
+        return slot >= 0 && (slot >> shift) < p.n_pages ? slot : -1;
+    };
+    const int slot = lane <= ROWS + C8_BLOCK ? block_of(t) : -1;
+    const int before = __shfl_up(slot, 1), at_first = t0 > 0 ? block_of(t0 - 1) : -1;
+    const unsigned long long changes = __ballot((lane == 0 ? at_first : before) >> 4 != slot >> 4);     // (-1 >> 4 is no block)
+    unsigned long long todo = changes & __ballot(slot >= 0 && lane < ROWS);
+    const elem* const src = (const elem*)p.src[which] + h * p.st[which][1] + 8 * sub;
+    while (todo) {
+        const int r0 = __ffsll((long long)todo) - 1;
+        todo &= todo - 1;
+        const unsigned long long behind = changes >> r0 >> 1;
+        const int rows = min(behind ? __ffsll((long long)behind) : 64, C8_BLOCK);           // of this run (more: slots that differ not)
+        vec x[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int k = min(i * AT_ONCE + rsel, rows - 1);                                // (a row once more in place of one that is not there)
+            x[i] = *(const vec*)(src + (t0 + r0 + k) * p.st[which][0]);
+        }
+        const int s0 = __builtin_amdgcn_readlane(slot, r0);
+        unsigned char* const part = p.cache + ((long)(s0 >> shift) * p.Hk + h) * cache8_part_bytes(D, shift);
+        const int block = (s0 & ((1 << shift) - 1)) / C8_BLOCK;
+        float* const scale_at = cache8_scale(part, D, shift, which, block);
+        unsigned char* const codes = part + ((which * D) << shift) + block * C8_BLOCK * D + 8 * sub;
+        // the lowest of the run's rows in the block, bit by bit
+        unsigned long long low = __ballot(lane >= r0 && lane < r0 + rows);
+        int first = 0;
+#pragma unroll
+        for (int bit = 3; bit >= 0; --bit) {
+            const unsigned long long zero = __ballot(!(slot >> bit & 1)) & low;
+            if (zero) low = zero; else first |= 1 << bit;
+        }
+        const float was = first ? *scale_at : 0.f;
+        float top = 0.f;
+        bool strange = false;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float a = fabsf((float)x[i][e]);
+                strange |= !(a < INFINITY);
+                top = fmaxf(top, a < INFINITY ? a : 0.f);
+            }
+        top = __uint_as_float((unsigned int)wave_max((int)__float_as_uint(top)));           // (bits of positive floats order like them)
+        strange = __any(strange) || __float_as_uint(was) >> 31;
+        const float old = fabsf(was), need = top > 0.f ? fmaxf(top / 127.f, 0x1p-126f) : 0.f;
+        const bool grown = !(old >= need && old < INFINITY);
+        const float s = grown ? need : old, inv = s > 0.f ? 1.f / s : 0.f;
+        if (grown && first) {
+            const double ratio_of = (double)(old < INFINITY ? old : 0.f);
+            for (int k = rsel; k < first; k += AT_ONCE) {
+                unsigned int* const at = (unsigned int*)(codes + k * D);
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const unsigned int c = at[w];
+                    unsigned int out = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int v = (signed char)(c >> (8 * e));
+                        const int n = v == -128 ? v : (int)rint((double)v * ratio_of / (double)s);
+                        out |= (unsigned int)(n & 255) << (8 * e);
+                    }
+                    at[w] = out;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int k = i * AT_ONCE + rsel;
+            unsigned int out[2] = {0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = (float)x[i][e];
+                const int n = fabsf(v) < INFINITY ? nearest_code(v, s, inv) : -128;
+                out[e >> 2] |= (unsigned int)(n & 255) << (8 * (e & 3));
+            }
+            const int row = __shfl(slot, r0 + min(k, rows - 1)) & (C8_BLOCK - 1);
+            if (k < rows) *(uint2*)(codes + row * D) = uint2{out[0], out[1]};
+        }
+        if (lane == 0 && (grown || !first || strange)) *scale_at = strange ? -s : s;
+    }
+}
+
+template <class E, int D, int U>
+__global__ __launch_bounds__(256) void cache8_read_kernel(RowParams p, unsigned int items) {
+    using elem = typename E::elem;
+    typedef elem vec __attribute__((ext_vector_type(8)));
+    const unsigned int first = blockIdx.x * (256u * U) + threadIdx.x;
+    RowItem r[U];
+    uint2 codes[U];
+    float scale[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = row_item<D>(p, first + 256u * u, items);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int slot = r[u].on ? r[u].slot : 0, row = slot & ((1 << p.page_shift) - 1);
+        const unsigned char* const part = p.cache + ((long)(slot >> p.page_shift) * p.Hk + r[u].h) * cache8_part_bytes(D, p.page_shift);
+        codes[u] = *(const uint2*)(part + ((r[u].which * D) << p.page_shift) + row * D + 8 * r[u].sub);
+        scale[u] = *cache8_scale(part, D, p.page_shift, r[u].which, row / C8_BLOCK);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float v[8];
+        cache8_expand(codes[u], __float_as_uint(scale[u]) >> 31, v);
+        vec y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (elem)(v[e] * fabsf(scale[u]));
+        if (r[u].on) *(vec*)((elem*)p.dst[r[u].which] + r[u].t * p.st[r[u].which][0] + r[u].h * p.st[r[u].which][1] + 8 * r[u].sub) = y;
+    }
+}
+
 }  // namespace ea
 
 namespace {
@@ -314,21 +445,27 @@ RowParams row_params(void* cache, const int32_t* slots, const int64_t* ks, const
     p.T = T; p.Hk = Hk; p.page_shift = cache_page_shift(page); p.n_pages = n_pages;
     return p;
 }
-template <bool WRITE, class E, int D, int U> void rows_launch(const RowParams& p, unsigned int items, hipStream_t s) {
+enum RowsCall { WRITE4, READ4, READ8 };
+template <RowsCall CALL, class E, int D, int U> void rows_launch(const RowParams& p, unsigned int items, hipStream_t s) {
     const dim3 grid((unsigned int)(((long)items + 256 * U - 1) / (256 * U)));
-    if constexpr (WRITE) hipLaunchKernelGGL((cache4_write_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
-    else hipLaunchKernelGGL((cache4_read_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
+    if constexpr (CALL == WRITE4) hipLaunchKernelGGL((cache4_write_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
+    else if constexpr (CALL == READ4) hipLaunchKernelGGL((cache4_read_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
+    else hipLaunchKernelGGL((cache8_read_kernel<E, D, U>), grid, dim3(256), 0, s, p, items);
 }
-template <bool WRITE> int rows_run(const RowParams& p, int d, int dtype, hipStream_t s) {
+template <RowsCall CALL> int rows_run(const RowParams& p, int d, int dtype, hipStream_t s) {
     const unsigned int items = (unsigned int)((long)p.T * 2 * p.Hk * (d / 8));
     const bool many = items >= ROWS_MANY;
     auto pick = [&](auto e) {
         using E = decltype(e);
-        if (d == 64) { if (many) rows_launch<WRITE, E, 64, 4>(p, items, s); else rows_launch<WRITE, E, 64, 1>(p, items, s); }
-        else { if (many) rows_launch<WRITE, E, 128, 4>(p, items, s); else rows_launch<WRITE, E, 128, 1>(p, items, s); }
+        if (d == 64) { if (many) rows_launch<CALL, E, 64, 4>(p, items, s); else rows_launch<CALL, E, 64, 1>(p, items, s); }
+        else { if (many) rows_launch<CALL, E, 128, 4>(p, items, s); else rows_launch<CALL, E, 128, 1>(p, items, s); }
     };
     if (dtype == EA_BF16) pick(Bf16{}); else pick(F32{});
     return launched();
+}
+template <class E, int D, int ROWS> void write8_launch(const RowParams& p, hipStream_t s) {
+    const unsigned int waves = (unsigned int)(((long)p.T + ROWS - 1) / ROWS * 2 * p.Hk);
+    hipLaunchKernelGGL((cache8_write_kernel<E, D, ROWS>), dim3(waves / 4 + (waves % 4 != 0)), dim3(256), 0, s, p, waves);
 }
 
 }  // namespace
@@ -365,7 +502,7 @@ int entmax_attn_cache4_write(const void* K, const void* V, const int64_t* k_stri
     if (T == 0) return EA_OK;
     RowParams p = row_params(cache, slots, k_strides, v_strides, T, Hk, page_size, n_pages);
     p.src[0] = K; p.src[1] = V;
-    return rows_run<true>(p, d, dtype, (hipStream_t)hip_stream);
+    return rows_run<WRITE4>(p, d, dtype, (hipStream_t)hip_stream);
 }
 
 int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
@@ -375,7 +512,40 @@ int entmax_attn_cache4_read(const void* cache, const int32_t* slots, void* K, vo
     if (T == 0) return EA_OK;
     RowParams p = row_params(const_cast<void*>(cache), slots, k_strides, v_strides, T, Hk, page_size, n_pages);
     p.dst[0] = K; p.dst[1] = V;
-    return rows_run<false>(p, d, dtype, (hipStream_t)hip_stream);
+    return rows_run<READ4>(p, d, dtype, (hipStream_t)hip_stream);
+}
+
+size_t entmax_attn_cache8_page_bytes(int Hk, int d, int page_size) {
+    if (!cache_shape_ok(Hk, d, page_size, 1)) return 0;
+    return (size_t)Hk * cache8_part_bytes(d, cache_page_shift(page_size));
+}
+
+int entmax_attn_cache8_write(const void* K, const void* V, const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                             void* cache, int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream) {
+    const int rc = rows_check(K, V, k_strides, v_strides, slots, cache, T, Hk, d, dtype, n_pages, page_size, false);
+    if (rc) return rc;
+    if (T == 0) return EA_OK;
+    RowParams p = row_params(cache, slots, k_strides, v_strides, T, Hk, page_size, n_pages);
+    p.src[0] = K; p.src[1] = V;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const bool few = (long)T * 2 * Hk <= C8_FEW;
+    auto pick = [&](auto e) {
+        using E = decltype(e);
+        if (d == 64) { if (few) write8_launch<E, 64, 1>(p, s); else write8_launch<E, 64, 16>(p, s); }
+        else { if (few) write8_launch<E, 128, 1>(p, s); else write8_launch<E, 128, 16>(p, s); }
+    };
+    if (dtype == EA_BF16) pick(Bf16{}); else pick(F32{});
+    return launched();
+}
+
+int entmax_attn_cache8_read(const void* cache, const int32_t* slots, void* K, void* V, const int64_t* k_strides, const int64_t* v_strides,
+                            int T, int Hk, int d, int dtype, int n_pages, int page_size, void* hip_stream) {
+    const int rc = rows_check(K, V, k_strides, v_strides, slots, cache, T, Hk, d, dtype, n_pages, page_size, true);
+    if (rc) return rc;
+    if (T == 0) return EA_OK;
+    RowParams p = row_params(const_cast<void*>(cache), slots, k_strides, v_strides, T, Hk, page_size, n_pages);
+    p.dst[0] = K; p.dst[1] = V;
+    return rows_run<READ8>(p, d, dtype, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

@@ -8,6 +8,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "pages.hpp"
 #include "tiles.hpp"
 
 namespace ea {
@@ -16,9 +17,5 @@ namespace ea {
 EA_DEV float cache4_scale(unsigned int byte) { return byte == 255u ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 1u << 22); }
 
 constexpr int cache_page_bytes(int d, int page) { return page * 2 * (d / 2 + d / 32); }   // of one head's part
-
-// Slots are 32-bit: token `slot % page` of page `slot / page`.
-inline bool cache_page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128 || page == 256; }
-inline int cache_page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : 8; }
 
 }  // namespace ea
