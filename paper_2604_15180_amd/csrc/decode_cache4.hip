@@ -27,7 +27,7 @@ namespace ea {
 
 // The cache as the kernel that gathers values takes it (paged_decode.hpp)
 struct Cache4 {
-    static constexpr bool WINDOWS = false;
+    static constexpr bool WINDOWS = false, PACKED = false;
     struct Piece { unsigned int codes; float scale; };            // eight values
     static EA_DEV Piece none() { return {0u, 0.f}; }
     template <int D> static EA_DEV long part_bytes(int shift) { return (long)(2 * (D / 2 + D / 32)) << shift; }

@@ -18,7 +18,7 @@ namespace ea {
 
 // The cache as the kernel that gathers values takes it (paged_decode.hpp)
 struct Cache8 {
-    static constexpr bool WINDOWS = true;
+    static constexpr bool WINDOWS = true, PACKED = true;
     struct Piece { uint2 codes; float scale; };                   // eight values
     static EA_DEV Piece none() { return {uint2{0u, 0u}, 0.f}; }
     template <int D> static EA_DEV long part_bytes(int shift) { return cache8_part_bytes(D, shift); }
@@ -87,7 +87,7 @@ EA_DEV void query_digits(const QRow<E, D>& row, int wave, int (*words)[8][64], f
 // 4 g .. 4 g + 3.  A wave keeps two blocks of 64 keys on their way: as soon as the matrix cores have taken a tile, the same tile of the
 // block after the next is requested.  The addresses and scales of all its tiles are formed and loaded at once, a lane for each.
 template <class E, int D>
-__global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParams p) {
+__global__ __launch_bounds__(64 * PD_WAVES, 3) void cache8_scores_kernel(PagedParams p) {
     constexpr int NT = sizeof(typename E::elem) == 2 ? 3 : 4, RUNS = D / 64, U = PD_BLOCK / 16;
     __shared__ unsigned int smax[16];                       // ordered bits of the work-group's running maxima
     __shared__ int words[NT][8][64];
@@ -125,9 +125,9 @@ __global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParam
     const unsigned char* const page = p.cache + ((long)id * p.Hk + kvh) * part_bytes;
     const uint64_t rows16 = (uint64_t)(page + (key16 & in_page) * D);
     const float scale16 = wanted ? *cache8_scale(page, D, shift, 0, (key16 & in_page) / C8_BLOCK) : 0.f;
-    float* const scores = p.scores + head * p.stride;
-    float* const bmax = p.bmax + head * (p.stride / PD_BLOCK);
-    const unsigned int lrow = n * D + 16 * g;
+    float* const room = p.scores + head * p.stride + first * PD_BLOCK;
+    PagedBlock* const found = p.found + head * (p.stride / PD_BLOCK);
+    const unsigned int lrow = RUNS == 2 ? (n & 7) * D + 64 * (n >> 3) + 16 * g : n * D + 16 * g;
     struct Batch { i32x4 a[U][RUNS]; };
     typedef const unsigned char __attribute__((address_space(1)))* global_bytes;       // (a pointer from two integers is not known to be global)
     typedef const i32x4 __attribute__((address_space(1)))* global_codes;
@@ -136,11 +136,22 @@ __global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParam
         const global_bytes rows = (global_bytes)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(rows16 >> 32), l) << 32 |
                                                  (uint32_t)__builtin_amdgcn_readlane((int)rows16, l));
 #pragma unroll
-        for (int run = 0; run < RUNS; ++run) x.a[u][run] = __builtin_nontemporal_load((global_codes)(rows + lrow + 64 * run));
+        for (int run = 0; run < RUNS; ++run) x.a[u][run] = __builtin_nontemporal_load((global_codes)(rows + lrow + 1024 * run));
+    };
+    auto operands = [&](i32x4 (&a)[RUNS]) {
+        if constexpr (RUNS == 2) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int lo = a[0][w], hi = a[1][w];
+                a[0][w] = __builtin_amdgcn_update_dpp(lo, hi, 0x128, 0xf, 0xc, false);
+                a[1][w] = __builtin_amdgcn_update_dpp(hi, lo, 0x128, 0xf, 0x3, false);
+            }
+        }
     };
     QDigits<D, NT> q;
     bool odd, bad;                                          // the lane's query is not finite; a score may not be
     float lmax = -INFINITY;
+    unsigned int kept = wave * paged_room(last - first);    // where the lane's head has its next four
     auto compute = [&](auto more, Batch& x, int i) {
         const int b = block_at(i), t0 = first_key(b);
         const bool whole = t0 + PD_BLOCK <= vis.sinks || (t0 >= vis.low && t0 + PD_BLOCK <= len);
@@ -150,6 +161,7 @@ __global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParam
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const float scale = __uint_as_float((unsigned int)__builtin_amdgcn_readlane((int)__float_as_uint(scale16), 4 * i + u));
+            operands(x.a[u]);
             i32x4 acc[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -168,7 +180,7 @@ __global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParam
                     }
                 nan |= any && seen(t0 + 16 * u + n);
             }
-            if constexpr (decltype(more)::value) load(x, i + 2, u);
+            if constexpr (decltype(more)::value) load(x, i + 1, u);
             const float unit = fabsf(scale) * q.unit;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -176,47 +188,51 @@ __global__ __launch_bounds__(64 * PD_WAVES) void cache8_scores_kernel(PagedParam
                 s[u][k] = fmaf((float)hi, 16384.f, (float)lo) * unit;
             }
         }
+        float quad[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 4; ++k)
                 if (!whole && !seen(t0 + 16 * u + 4 * g + k)) s[u][k] = -INFINITY;
-                best = fmaxf(best, s[u][k]);
-            }
+            quad[u] = fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3]));
+            best = fmaxf(best, quad[u]);
+        }
         best = across16_max(best);
         if (bad || __any(nan)) best = INFINITY;
         if (!live) best = -INFINITY;
         const float shared_max = from_ordered_bits(__hip_atomic_load(&smax[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         lmax = fmaxf(lmax, best);
         const float m = fmaxf(lmax, shared_max);
-        if (live && g == 0) bmax[b] = best;
         // (a maximum that is infinite: NaN, nothing is kept, nor is anything needed)
-        const bool keep = best >= m - p.win - 1e-6f * fabsf(m) && live;
-        if (!__any(keep)) return;
-        if (g == 0 && best > shared_max) atomicMax(&smax[n], ordered_bits(best));
-        if (keep) {
+        const float low = m - p.win - 1e-6f * fabsf(m);
+        unsigned int fours = 0;
+        const unsigned int before = kept;
+        if (__any(best >= low && live)) {
+            if (g == 0 && best > shared_max) atomicMax(&smax[n], ordered_bits(best));
 #pragma unroll
-            for (int u = 0; u < U; ++u) *(f32x4*)(scores + b * PD_BLOCK + 16 * u + 4 * g) = s[u];
+            for (int u = 0; u < U; ++u) fours |= (quad[u] >= low && live) << (4 * u + g);
+            fours = across16_or(fours);
+            kept += __popc(fours);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const unsigned int k = before + __popc(fours & ((1u << (4 * u + g)) - 1u));
+                if (quad[u] >= low && live) *(f32x4*)(room + 4 * k) = s[u];
+            }
         }
+        if (live && g == 0) found[b] = PagedBlock{best, (unsigned short)fours, (unsigned short)before};
     };
     constexpr auto more = std::true_type{};
     constexpr auto no_more = std::false_type{};
-    Batch x0, x1;
+    Batch x0;
 #pragma unroll
     for (int u = 0; u < U; ++u) if (mine > 0) load(x0, 0, u);
-#pragma unroll
-    for (int u = 0; u < U; ++u) if (mine > 1) load(x1, 1, u);
     query_digits<E, D, NT>(qrow, wave, words, tops, q, odd);
     // |score| < 2^21 * 2^14 (three terms; 2^28 * 2^14) * unit * scale, and unit holds 2^-14 (2^-21): at most 2^22 * 2^(e - 6) * scale
     const float most = whole_wave_max(wanted ? (fabsf(scale16) < INFINITY ? fabsf(scale16) : INFINITY) : 0.f);
     bad = odd || __any(strange) || !(most < INFINITY) || !(most * q.unit < (NT == 3 ? 0x1p84f : 0x1p77f));
     int i = 0;
-    for (; i + 3 < mine; i += 2) { compute(more, x0, i); compute(more, x1, i + 1); }
-    if (i + 2 < mine) { compute(more, x0, i); compute(no_more, x1, i + 1); compute(no_more, x0, i + 2); }
-    else {
-        if (i < mine) compute(no_more, x0, i);
-        if (i + 1 < mine) compute(no_more, x1, i + 1);
-    }
+    for (; i + 1 < mine; ++i) compute(more, x0, i);
+    if (i < mine) compute(no_more, x0, i);
 }
 
 template <class E, int D>
@@ -244,14 +260,17 @@ int cache8_span(int max_len, int window, int sinks) {
     return (int)(some < all ? some : all) * PD_BLOCK;
 }
 
+// (three blocks for the waves' quarters: paged_room)
+long cache8_stride(int span) { return paged_stride(span + 3 * PD_BLOCK); }
+
 }  // namespace
 
 extern "C" {
 
 size_t entmax_attn_decode_cache8_workspace_bytes(int R, int Hq, int Hk, int d, int max_len, int window, int sinks) {
     if (!cache8_decode_shape_ok(R, Hq, Hk, d, max_len, window, sinks)) return 0;
-    const size_t keys = (size_t)R * Hq * paged_stride(cache8_span(max_len, window, sinks));
-    return align256(keys * 4) + align256(keys / PD_BLOCK * 4);
+    const size_t keys = (size_t)R * Hq * cache8_stride(cache8_span(max_len, window, sinks));
+    return align256(keys * 4) + align256(keys / PD_BLOCK * sizeof(PagedBlock));
 }
 
 int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* block_table, const int32_t* lens,
@@ -272,13 +291,15 @@ int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* b
     p.q = q; p.cache = (const unsigned char*)cache; p.table = block_table; p.lens = lens;
     p.O = O; p.tau = tau; p.support = support;
     p.span = cache8_span(max_len, window, sinks);
-    p.stride = paged_stride(p.span);
+    p.stride = cache8_stride(p.span);
     p.scores = (float*)workspace;
-    p.bmax = (float*)((char*)workspace + align256((size_t)R * Hq * p.stride * 4));
+    p.found = (PagedBlock*)((char*)workspace + align256((size_t)R * Hq * p.stride * 4));
     p.R = R; p.Hq = Hq; p.Hk = Hk; p.G = Hq / Hk; p.colgroups = (p.G + 15) / 16;
     p.blocks = max_blocks; p.n_pages = n_pages; p.page_shift = cache_page_shift(page_size); p.max_len = max_len;
     p.window = window; p.sinks = sinks;
     p.part = paged_part(R, Hq, Hk, p.span);
+    p.group = PD_WAVES * p.part / PD_BLOCK;
+    p.by_group = (unsigned int)((1ull << 32) / p.group) + 1u;
     p.alpha = alpha; p.r = 1.f / (alpha - 1.f);
     p.c64 = ((double)alpha - 1.0) / sqrt((double)d);
     p.c = (float)p.c64;

@@ -16,13 +16,27 @@ constexpr int PD_WAVES = 4;             // waves per work-group of a score kerne
 constexpr int PD_BLOCK = 64;            // keys per maximum
 constexpr int PD_MAX_PART = 512;        // keys per wave of a score kernel, at most
 
+// What a score kernel leaves of 64 keys and a head for the second kernel.
+// The 4-bit cache's (not Cache::PACKED): their maximum in bmax (+inf also where a score is not a number or a page id out of range), and at
+// their own places in scores all 64, where one of them was within the window of Eq. 5 under the largest score its wave knew.
+// The 8-bit cache's (PACKED): the maximum, and a bit for each four neighbouring keys of which one was in that window.  The scores of these
+// fours alone are written: each wave of a work-group packs those of a head, one behind the other, into a quarter (paged_room) of the
+// room that the work-group's keys have; `before` lie in front of the block's, counted from the room's beginning.
+// Keys in the window are few and far between, and a store costs the same whether it fills a line or not: with whole blocks the stores took 14 of
+// 68 us for 48 requests up to 32768 keys, now 9 of 63, and 7 of 99 for one of 131072 with 32 key heads, now 1; unpacked fours were no faster
+// than blocks.  The second kernel takes 0.5 to 1 us more, which is what the 4-bit cache would gain, whose keys are half the bytes.
+struct alignas(8) PagedBlock { float max; unsigned short fours, before; };
+// fours of a wave's quarter, of a work-group with so many blocks (together up to three blocks more than those)
+EA_DEV unsigned int paged_room(int blocks) { return (blocks + PD_WAVES - 1) / PD_WAVES * (PD_BLOCK / 4); }
+
 struct PagedParams {
     const void* q; const unsigned char* cache; const int32_t* table; const int32_t* lens;
     float* O; float* tau; int32_t* support;
-    float* scores;            // [R][Hq][stride]: s_j, where a block's maximum was in the window (else whatever stood there)
-    float* bmax;              // [R][Hq][stride / 64]: maximum of 64 keys; +inf also where a score is not a number or a page id out of range
+    float* scores;            // [R][Hq][stride]
+    float* bmax; PagedBlock* found;     // [R][Hq][stride / 64], one of them: see PagedBlock
     long stride;              // keys a head has room for (paged_stride)
     int part;                 // keys per wave of the score kernel, a multiple of 64
+    int group; unsigned int by_group;   // (PACKED) blocks of its work-group; 2^32 / group, rounded up: the upper half of a block's number (below 2^17) times it is the group's
     int R, Hq, Hk, G, colgroups;        // G = Hq / Hk query heads per key head, in colgroups of up to 16
     int blocks, n_pages, page_shift, max_len;
     int window, sinks;        // (8-bit cache) keys a query sees: the last `window` and the first `sinks`; window 0: all
@@ -59,6 +73,12 @@ EA_DEV float across16_max(float v) {
     v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+EA_DEV unsigned int across16_or(unsigned int v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = a[0] | a[1];
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return b[0] | b[1];
 }
 EA_DEV float whole_wave_max(float v) {
     v = fmaxf(v, dpp_move<0xB1>(v));
@@ -113,11 +133,14 @@ __global__ __launch_bounds__(64 * NW) void paged_entmax_kernel(PagedParams p) {
     const int nblocks = vis.count, per = (nblocks + NW - 1) / NW;
     const int b0 = min(wave * per, nblocks), b1 = min(b0 + per, nblocks);
     const float* scores = p.scores + head * p.stride;
-    const float* bmax = p.bmax + head * (p.stride / PD_BLOCK);
+    auto block_max = [&](int b) {
+        if constexpr (C::PACKED) return p.found[head * (p.stride / PD_BLOCK) + b].max;
+        else return p.bmax[head * (p.stride / PD_BLOCK) + b];
+    };
     const float r = p.r;
 
     float gm = -INFINITY;
-    for (int b = b0 + lane; b < b1; b += 64) gm = fmaxf(gm, bmax[b]);
+    for (int b = b0 + lane; b < b1; b += 64) gm = fmaxf(gm, block_max(b));
     gm = whole_wave_max(gm);
     if (lane == 0) red[0][wave][0] = gm;
     __syncthreads();
@@ -131,22 +154,46 @@ __global__ __launch_bounds__(64 * NW) void paged_entmax_kernel(PagedParams p) {
         if (tid == 0 && slice == 0) { p.tau[head] = v; if (p.support) p.support[head] = len == 0 ? 0 : -1; }
         return;
     }
+    // A lane for each of 64 blocks from c0 on: whether it reaches into the window, and where what was left of its scores begins; of a
+    // packed block's which fours
+    struct Left { int at; unsigned int fours; bool in; };
+    auto left_of = [&](int c0) {
+        const int b = min(c0 + lane, b1 - 1);
+        if constexpr (C::PACKED) {
+            const PagedBlock x = p.found[head * (p.stride / PD_BLOCK) + b];
+            const bool in = c0 + lane < b1 && p.c * (x.max - gm) >= -1.f;
+            return Left{(int)__umulhi((unsigned int)b, p.by_group) * p.group * PD_BLOCK + 4 * x.before, in ? x.fours : 0u, in};
+        } else {
+            return Left{0, 0u, c0 + lane < b1 && p.c * (block_max(b) - gm) >= -1.f};
+        }
+    };
     // f(x, key) for the scores of the wave's blocks that reach into the window, in the order of their keys, a block at a time, four
     // such loads in flight, and then after(); every 64 blocks enough() may end it (asked after every load, 1 us more for 48 requests up
-    // to 32768 keys).  (The score kernel has written these blocks: its window was this one or a lower one.)
+    // to 32768 keys).  (What the score kernel has not written is below the window: its own was this one or a lower one.)
+    const unsigned int below = (1u << (lane >> 2)) - 1u;
     auto walk = [&](auto f, auto after, auto enough) {
         for (int c0 = b0; c0 < b1; c0 += 64) {
-            unsigned long long todo = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
+            const Left left = left_of(c0);
+            unsigned long long todo = __ballot(left.in);
             while (todo) {
                 float s[U];
                 int key[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     key[u] = -1;
+                    if constexpr (C::PACKED) s[u] = -INFINITY;
                     if (!todo) continue;
-                    key[u] = (c0 + __ffsll((long long)todo) - 1) * PD_BLOCK;
+                    const int i = __ffsll((long long)todo) - 1;
+                    key[u] = (c0 + i) * PD_BLOCK;
                     todo &= todo - 1;
-                    s[u] = scores[key[u] + lane];
+                    if constexpr (C::PACKED) {
+                        const unsigned int fours = (unsigned int)__builtin_amdgcn_readlane((int)left.fours, i);
+                        const int at = __builtin_amdgcn_readlane(left.at, i);
+                        // (the other lanes load nothing: with addresses of their own for no use 1 to 2 us more)
+                        if (fours >> (lane >> 2) & 1) s[u] = scores[at + 4 * __popc(fours & below) + (lane & 3)];
+                    } else {
+                        s[u] = scores[key[u] + lane];
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -159,14 +206,22 @@ __global__ __launch_bounds__(64 * NW) void paged_entmax_kernel(PagedParams p) {
     // The same for sums alone: g(x) for all of them, 256 keys a load.
     auto stream = [&](auto g) {
         for (int c0 = b0; c0 < b1; c0 += 64) {
-            const unsigned long long in = __ballot(c0 + lane < b1 && p.c * (bmax[min(c0 + lane, b1 - 1)] - gm) >= -1.f);
+            const Left left = left_of(c0);
+            const unsigned long long in = __ballot(left.in);
 #pragma unroll 1
             for (int j = 0; j < 16; j += U) {
                 f32x4 v[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     v[u] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    if (in >> (4 * (j + u) + (lane >> 4)) & 1) v[u] = *(const f32x4*)(scores + (c0 + 4 * (j + u)) * PD_BLOCK + 4 * lane);
+                    const int i = 4 * (j + u) + (lane >> 4);                    // (the lane's block)
+                    if constexpr (C::PACKED) {
+                        const unsigned int fours = __shfl(left.fours, i);
+                        const int at = __shfl(left.at, i);
+                        if (fours >> (lane & 15) & 1) v[u] = *(const f32x4*)(scores + at + 4 * __popc(fours & ((1u << (lane & 15)) - 1u)));
+                    } else {
+                        if (in >> i & 1) v[u] = *(const f32x4*)(scores + (c0 + 4 * (j + u)) * PD_BLOCK + 4 * lane);
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
