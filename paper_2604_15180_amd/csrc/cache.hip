@@ -3,6 +3,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache4.hpp"
 #include "cache8.hpp"
 #include "common.hpp"
@@ -275,16 +277,32 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
 // larger than the block's: then it becomes the block's, and they are rounded once more.  A run that begins with row 0
 // begins its block.
 // The nearest integer n is that of x times 1 / s, which is off by up to 2^-16; the remainder x - n s, exact in one fused
-// multiply-add, then tells whether n is the one (halves are exact, too).  Kept codes are rounded in 64 bits, where c s_old is exact.
+// multiply-add, then tells whether n is the one (halves are exact, too).  It hardly ever is not, nor is a value: both are looked at
+// for all of a lane's values at once, and put right in a branch of their own.  Kept codes: c s_old = p + e with two floats, and
+// likewise.
 
-constexpr int C8_FEW = 1 << 15;         // waves up to which a wave looks after one token's run
+// Tokens whose runs a wave looks after: 1 up to C8_FEW (tokens x heads of keys and values), 4 up to C8_MANY, 16 above.  One each keeps the
+// waves short, but of a prompt's only each sixteenth finds a run.  us with 1 / 4 / 16 tokens, 8 key heads of 128: 1400 requests with a token each
+// (22400) 16.7 / 16.2 / 25.3, 4000 (64000) 47.3 / 38.6 / 40.0; 8 chunks of 512 (50000) 22.0 / 13.4 / 10.4; chunks of 127, 5 heads of 64 (23000)
+// 7.4 / 6.0 / 6.0.
+constexpr int C8_FEW = 1 << 12, C8_MANY = 1 << 15;
 
-// The integer in -127 .. 127 nearest to x / s, ties to even; |x| <= 127 s (1 + 2^-24), inv = 1 / s
-EA_DEV int nearest_code(float x, float s, float inv) {
-    float n = rintf(x * inv);
-    const float rest = fmaf(-n, s, x), twice = 2.f * fabsf(rest);
-    if (twice > s || (twice == s && ((int)n & 1))) n += copysignf(1.f, rest);
-    return (int)fminf(fmaxf(n, -127.f), 127.f);
+// The float whose lowest byte is the nearest integer to x * inv, |x * inv| < 2^22; less C8_MAGIC it is that integer
+constexpr float C8_MAGIC = 12582912.f;          // 1.5 * 2^23
+EA_DEV float c8_near(float x, float inv) { return fmaf(x, inv, C8_MAGIC); }
+// The lowest bytes of four, in order
+EA_DEV unsigned int c8_bytes(const float* m) {
+    const unsigned int lo = __builtin_amdgcn_perm(__float_as_uint(m[1]), __float_as_uint(m[0]), 0x0c0c0400u);
+    const unsigned int hi = __builtin_amdgcn_perm(__float_as_uint(m[3]), __float_as_uint(m[2]), 0x0c0c0400u);
+    return hi << 16 | lo;
+}
+// n, an integer one of the two next to x / s, where x = p + e (e far below s): the nearest, ties to the even one
+EA_DEV float c8_put_right(float n, float p, float e, float s) {
+    const float rest = fmaf(-n, s, p), side = copysignf(1.f, rest);
+    // 2 |x - n s| - s: both sums are exact next to zero and have the right sign elsewhere
+    const float over = fmaf(2.f * side, e, 2.f * fabsf(rest) - s);
+    if (over > 0.f || (over == 0.f && ((int)n & 1))) n += side;
+    return fminf(fmaxf(n, -127.f), 127.f);
 }
 
 template <class E, int D, int ROWS>
@@ -296,14 +314,14 @@ __global__ __launch_bounds__(256) void cache8_write_kernel(RowParams p, unsigned
     if (id >= waves) return;
     const int lane = threadIdx.x & 63, sub = lane % LPR, rsel = lane / LPR;
     const int t0 = (int)(id / per) * ROWS, which = id % per >= (unsigned int)p.Hk, h = (int)(id % per) - (which ? p.Hk : 0);
-    // lane k: the row before t0 + k and this one.  Runs begin where the block changes (or the call does).
+    // lane k: row t0 + k.  Runs begin where the block changes (or the call does).
     const int shift = p.page_shift, t = t0 + lane;
-    auto block_of = [&](int row) {
+    auto slot_of = [&](int row) {
         const int slot = row >= 0 && row < p.T ? p.slots[row] : -1;
         return slot >= 0 && (slot >> shift) < p.n_pages ? slot : -1;
     };
-    const int slot = lane <= ROWS + C8_BLOCK ? block_of(t) : -1;
-    const int before = __shfl_up(slot, 1), at_first = t0 > 0 ? block_of(t0 - 1) : -1;
+    const int slot = lane <= ROWS + C8_BLOCK ? slot_of(t) : -1;
+    const int before = __shfl_up(slot, 1), at_first = t0 > 0 ? slot_of(t0 - 1) : -1;
     const unsigned long long changes = __ballot((lane == 0 ? at_first : before) >> 4 != slot >> 4);     // (-1 >> 4 is no block)
     unsigned long long todo = changes & __ballot(slot >= 0 && lane < ROWS);
     const elem* const src = (const elem*)p.src[which] + h * p.st[which][1] + 8 * sub;
@@ -331,52 +349,79 @@ __global__ __launch_bounds__(256) void cache8_write_kernel(RowParams p, unsigned
             const unsigned long long zero = __ballot(!(slot >> bit & 1)) & low;
             if (zero) low = zero; else first |= 1 << bit;
         }
-        const float was = first ? *scale_at : 0.f;
-        float top = 0.f;
-        bool strange = false;
+        // (asked for with the rows, whether they will be rounded again or not: 64 requests with a token each 1 us less)
+        float was = 0.f;
+        uint2 kept[STEPS];
+        if (first) {
+            was = *scale_at;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) kept[i] = *(const uint2*)(codes + min(i * AT_ONCE + rsel, first - 1) * D);
+        }
+        unsigned int bits = 0;                                                              // (of positive floats order like them)
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float a = fabsf((float)x[i][e]);
-                strange |= !(a < INFINITY);
-                top = fmaxf(top, a < INFINITY ? a : 0.f);
-            }
-        top = __uint_as_float((unsigned int)wave_max((int)__float_as_uint(top)));           // (bits of positive floats order like them)
-        strange = __any(strange) || __float_as_uint(was) >> 31;
-        const float old = fabsf(was), need = top > 0.f ? fmaxf(top / 127.f, 0x1p-126f) : 0.f;
-        const bool grown = !(old >= need && old < INFINITY);
+            for (int e = 0; e < 8; ++e) bits = max(bits, __float_as_uint((float)x[i][e]) & 0x7fffffffu);
+        bits = (unsigned int)wave_max((int)bits);
+        const bool odd = bits >= 0x7f800000u;                                               // some value is not finite
+        if (odd) {
+            bits = 0;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned int a = __float_as_uint((float)x[i][e]) & 0x7fffffffu;
+                    bits = max(bits, a < 0x7f800000u ? a : 0u);
+                }
+            bits = (unsigned int)wave_max((int)bits);
+        }
+        const float old = fabsf(was), need = bits ? fmaxf(__uint_as_float(bits) / 127.f, 0x1p-126f) : 0.f;
+        const bool grown = !(old >= need && old < INFINITY), strange = odd || __float_as_uint(was) >> 31;
         const float s = grown ? need : old, inv = s > 0.f ? 1.f / s : 0.f;
         if (grown && first) {
-            const double ratio_of = (double)(old < INFINITY ? old : 0.f);
-            for (int k = rsel; k < first; k += AT_ONCE) {
-                unsigned int* const at = (unsigned int*)(codes + k * D);
+            // (scales below 1 are taken up, so that no part of c s_old is lost where it counts)
+            const float up = s < 1.f ? 0x1p60f : 1.f, so = (old < INFINITY ? old : 0.f) * up, sn = s * up, in = 1.f / sn;
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const unsigned int c = at[w];
-                    unsigned int out = 0;
+            for (int i = 0; i < STEPS; ++i) {
+                if (i * AT_ONCE >= first) break;
+                const int k = i * AT_ONCE + rsel;
+                float m[8], far = 0.f;
+                auto code = [&](int e) { return (float)(signed char)((e >> 2 ? kept[i].y : kept[i].x) >> (8 * (e & 3))); };
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int v = (signed char)(c >> (8 * e));
-                        const int n = v == -128 ? v : (int)rint((double)v * ratio_of / (double)s);
-                        out |= (unsigned int)(n & 255) << (8 * e);
-                    }
-                    at[w] = out;
+                for (int e = 0; e < 8; ++e) {
+                    m[e] = c8_near(code(e) * so, in);
+                    far = fmaxf(far, fabsf(fmaf(C8_MAGIC - m[e], sn, code(e) * so)));
                 }
+                // (the products, up to 127 sn, are rounded by up to 2^-17 sn)
+                if (__any(2.f * far >= sn * (1.f - 0x1p-14f) || cache8_odd(kept[i].x) || cache8_odd(kept[i].y))) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float c = code(e), q = c * so;
+                        m[e] = (c == -128.f ? c : c8_put_right(m[e] - C8_MAGIC, q, fmaf(c, so, -q), sn)) + C8_MAGIC;
+                    }
+                }
+                if (k < first) *(uint2*)(codes + k * D) = uint2{c8_bytes(m), c8_bytes(m + 4)};
             }
         }
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
+            if (i * AT_ONCE >= rows) break;
             const int k = i * AT_ONCE + rsel;
-            unsigned int out[2] = {0u, 0u};
+            float m[8], far = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float v = (float)x[i][e];
-                const int n = fabsf(v) < INFINITY ? nearest_code(v, s, inv) : -128;
-                out[e >> 2] |= (unsigned int)(n & 255) << (8 * (e & 3));
+                m[e] = c8_near((float)x[i][e], inv);
+                far = fmaxf(far, fabsf(fmaf(C8_MAGIC - m[e], s, (float)x[i][e])));
+            }
+            if (odd || __any(2.f * far >= s)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = (float)x[i][e];
+                    m[e] = (fabsf(v) < INFINITY ? c8_put_right(m[e] - C8_MAGIC, v, 0.f, s) : -128.f) + C8_MAGIC;
+                }
             }
             const int row = __shfl(slot, r0 + min(k, rows - 1)) & (C8_BLOCK - 1);
-            if (k < rows) *(uint2*)(codes + row * D) = uint2{out[0], out[1]};
+            if (k < rows) *(uint2*)(codes + row * D) = uint2{c8_bytes(m), c8_bytes(m + 4)};
         }
         if (lane == 0 && (grown || !first || strange)) *scale_at = strange ? -s : s;
     }
@@ -528,13 +573,17 @@ int entmax_attn_cache8_write(const void* K, const void* V, const int64_t* k_stri
     RowParams p = row_params(cache, slots, k_strides, v_strides, T, Hk, page_size, n_pages);
     p.src[0] = K; p.src[1] = V;
     hipStream_t s = (hipStream_t)hip_stream;
-    const bool few = (long)T * 2 * Hk <= C8_FEW;
-    auto pick = [&](auto e) {
+    const long heads = (long)T * 2 * Hk;
+    auto pick = [&](auto e, auto rows) {
         using E = decltype(e);
-        if (d == 64) { if (few) write8_launch<E, 64, 1>(p, s); else write8_launch<E, 64, 16>(p, s); }
-        else { if (few) write8_launch<E, 128, 1>(p, s); else write8_launch<E, 128, 16>(p, s); }
+        if (d == 64) write8_launch<E, 64, decltype(rows)::value>(p, s); else write8_launch<E, 128, decltype(rows)::value>(p, s);
     };
-    if (dtype == EA_BF16) pick(Bf16{}); else pick(F32{});
+    auto rows = [&](auto e) {
+        if (heads <= C8_FEW) pick(e, std::integral_constant<int, 1>{});
+        else if (heads <= C8_MANY) pick(e, std::integral_constant<int, 4>{});
+        else pick(e, std::integral_constant<int, 16>{});
+    };
+    if (dtype == EA_BF16) rows(Bf16{}); else rows(F32{});
     return launched();
 }
 

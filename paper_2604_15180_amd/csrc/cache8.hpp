@@ -24,6 +24,11 @@ EA_DEV float* cache8_scale(unsigned char* part, int d, int shift, int which, int
 EA_DEV const float* cache8_scale(const unsigned char* part, int d, int shift, int which, int block) {
     return cache8_scale(const_cast<unsigned char*>(part), d, shift, which, block);
 }
+// Whether one of four codes is -128
+EA_DEV bool cache8_odd(unsigned int codes) {
+    const unsigned int y = codes ^ 0x80808080u;
+    return ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+}
 // Eight values in units of the scale; `strange`: codes -128 become NaN
 EA_DEV void cache8_expand(uint2 codes, bool strange, float* v) {
     const int w[2] = {(int)codes.x, (int)codes.y};

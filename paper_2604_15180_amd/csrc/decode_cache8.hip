@@ -174,10 +174,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, 3) void cache8_scores_kernel(PagedPa
 #pragma unroll
                 for (int run = 0; run < RUNS; ++run)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const unsigned int y = (unsigned int)x.a[u][run][w] ^ 0x80808080u;
-                        any |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
-                    }
+                    for (int w = 0; w < 4; ++w) any |= cache8_odd((unsigned int)x.a[u][run][w]);
                 nan |= any && seen(t0 + 16 * u + n);
             }
             if constexpr (decltype(more)::value) load(x, i + 1, u);

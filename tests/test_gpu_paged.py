@@ -83,6 +83,48 @@ def test_rows_of_a_long_prompt(ea, T, Hk, d, dtype):  # noqa: F811
     same_rows(got, want.read(slots), DT[dtype])
 
 
+def test_rows_of_many_requests(ea):  # noqa: F811
+    # a few tokens each for some hundred requests (the write's middle variant), three times over: scales grow in most blocks
+    Hk, d, page, R = 4, 64, 64, 300
+    rng = np.random.default_rng(12)
+    cache, want = pair(R * 2, Hk, d, page, seed=5)
+    order = rng.permutation(R * 2).reshape(R, 2)
+    at = np.zeros(R, np.int64)
+    for step in range(3):
+        chunk = rng.integers(0, 12, R)
+        slots = np.concatenate([order[r][np.arange(a, a + c) // page] * page + np.arange(a, a + c) % page for r, (a, c) in enumerate(zip(at, chunk))])
+        at += chunk
+        k, v = rows_of(rng, len(slots), Hk, d, "bf16") * (1 + step), rows_of(rng, len(slots), Hk, d, "bf16") / (1 + step)
+        assert 1 << 12 < len(slots) * 2 * Hk <= 1 << 15
+        ea.entmax_attn_cache8_write(k.cuda(), v.cuda(), i32(slots.tolist()), cache, page)
+        want.write(k.float().numpy(), v.float().numpy(), slots)
+        np.testing.assert_array_equal(cache.cpu().numpy(), want.bytes())
+
+
+def test_kept_rows_that_are_hard_to_round_again(ea):  # noqa: F811
+    """A block of scale s with every code, and rows whose scale is s times what makes halves of many codes (2, 4, 2/3 ...) or nearly so."""
+    d, page = 128, 32
+    codes = torch.arange(-127, 129).clamp(max=127).float().view(2, 1, d)
+    for s in (1.0, float(np.float32(1 / 3)), 2.0 ** -126, 1.7 * 2.0 ** -120, 1.9 * 2.0 ** 118):
+        for ratio in (2.0, 4.0, 4 / 3, 2 / 1.5, 254.0, 8.0, 1.0000001, 1.5, 600.0, 2.0 ** 20):
+            for step in (0, 1, -1):
+                with np.errstate(over="ignore"):
+                    top = np.float32(127) * np.float32(s) * np.float32(ratio)
+                for _ in range(abs(step) * 60):
+                    top = np.nextafter(top, np.float32(np.inf * step))
+                if not np.isfinite(top):
+                    continue
+                cache, want = pair(1, 1, d, page, seed=3)
+                k = codes * s
+                v = torch.from_numpy(np.random.default_rng(4).standard_normal((2, 1, d)).astype(np.float32))
+                row = torch.zeros(1, 1, d)
+                row[0, 0, 77] = float(top)
+                for a, b, slots in ((k, v, [16, 17]), (row, row, [18])):
+                    ea.entmax_attn_cache8_write(a.cuda(), b.cuda(), i32(slots), cache, page)
+                    want.write(a.numpy(), b.numpy(), slots)
+                    np.testing.assert_array_equal(cache.cpu().numpy(), want.bytes(), err_msg=str((s, ratio, step)))
+
+
 def test_rows_that_are_hard_to_round(ea):  # noqa: F811
     """Quotients at and next to halves, zeros, the smallest and largest values, infinities and NaN; a block that grows past all of it."""
     d, page = 64, 16
