@@ -50,19 +50,6 @@ EA_DEV void table_row(const TableParams& p, int t, int r, int start, int end, bo
     p.positions[t] = position;
 }
 
-// inclusive sum over the lanes up to this one, by data-parallel-primitive adds (through LDS each of the six steps waits for its
-// predecessor's round trip)
-template <int CTRL, int ROWS> EA_DEV int scan_step(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-EA_DEV int wave_scan(int v) {
-    v = scan_step<0x111, 0xf>(v);        // row_shr 1, 2, 4, 8: within sixteen lanes
-    v = scan_step<0x112, 0xf>(v);
-    v = scan_step<0x114, 0xf>(v);
-    v = scan_step<0x118, 0xf>(v);
-    v = scan_step<0x142, 0xa>(v);        // row_bcast 15: the row before, to the odd rows
-    v = scan_step<0x143, 0xc>(v);        // row_bcast 31: the lower half, to the upper one
-    return v;
-}
-
 __global__ __launch_bounds__(1024) void cache_tables_kernel(TableParams p) {
     constexpr int T = 1024, NW = T / 64;
     __shared__ int32_t left[TABLE_MAX_REQUESTS + 1], want[TABLE_MAX_REQUESTS + 1], start[TABLE_MAX_REQUESTS + 1];   // exclusive prefix sums

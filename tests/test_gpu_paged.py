@@ -475,7 +475,9 @@ class Shared:
         return out
 
 
-@pytest.mark.parametrize("R,blocks,page,pages", [(1, 4, 16, 10), (5, 8, 16, 60), (70, 12, 32, 900), (1100, 5, 16, 4000), (4096, 2, 64, 9000)])
+@pytest.mark.parametrize("R,blocks,page,pages", [(1, 4, 16, 10), (5, 8, 16, 60), (70, 12, 32, 900), (1100, 5, 16, 4000), (4096, 2, 64, 9000),
+                                                 # (in four launches)
+                                                 (1100, 30, 16, 20000), (40, 800, 16, 17000), (4096, 9, 32, 20000), (3, 6000, 16, 10000)])
 def test_forks_against_the_reference(ea, R, blocks, page, pages):  # noqa: F811
     rng = np.random.default_rng(R)
     s = Shared([int(n) for n in rng.integers(0, blocks * page // 2, R)], pages, blocks, page, rng)
@@ -485,18 +487,20 @@ def test_forks_against_the_reference(ea, R, blocks, page, pages):  # noqa: F811
     assert s.count.item() == pages and s.shares.sum().item() == 0 and sorted(s.free.tolist()) == list(range(pages))
 
 
-def test_forks_where_no_page_is_left(ea):  # noqa: F811
+@pytest.mark.parametrize("blocks", [4, 3000])                                # (one launch, four launches)
+def test_forks_where_no_page_is_left(ea, blocks):  # noqa: F811
     rng = np.random.default_rng(7)
-    s = Shared([40, 0, 0, 0, 33, 0], 8, 4, 16, rng, free=2)
+    s = Shared([40, 0, 0, 0, 33, 0], 8, blocks, 16, rng, free=2)
     out = s.fork(ea, [0, 0, 0, 4, 4, 4], [40, 40, 33, 33, 33, 32])           # copies for 1, 2 and 3, two pages left
     assert out[2].tolist() == [2, 1, 0, 0]
     s.fork(ea, list(range(6)), [0, 40 if s.lens[1] == 40 else s.lens[1], 0, 0, 0, 16])
 
 
-def test_forks_with_arguments_out_of_range(ea):  # noqa: F811
+@pytest.mark.parametrize("blocks", [4, 9000])
+def test_forks_with_arguments_out_of_range(ea, blocks):  # noqa: F811
     rng = np.random.default_rng(8)
-    lens = [40, -1, 65, 20, 0, 7]
-    s = Shared([40, 0, 0, 20, 0, 7], 20, 4, 16, rng)
+    lens = [40, -1, blocks * 16 + 1, 20, 0, 7]
+    s = Shared([40, 0, 0, 20, 0, 7], 20, blocks, 16, rng)
     s.lens = lens
     out = s.fork(ea, [6, 1, 2, -1, 0, 1], [3, 0, 10, 5, 41, 0])              # a parent that is none (twice), lengths of their own, above the parent's
     assert out[2].tolist() == [0, 0, 6, 0] and out[0].tolist() == lens
@@ -507,10 +511,11 @@ def test_forks_with_arguments_out_of_range(ea):  # noqa: F811
     assert out[2].tolist()[3] == 2
 
 
-def test_forks_as_lens_itself_and_captured(ea):  # noqa: F811
+@pytest.mark.parametrize("blocks", [10, 3000])
+def test_forks_as_lens_itself_and_captured(ea, blocks):  # noqa: F811
     # lens_out = lens and a workspace kept; captured once, replayed with other parents and lengths, eager work between
     rng = np.random.default_rng(9)
-    R, blocks, page, pages = 6, 10, 16, 80
+    R, page, pages = 6, 16, 80
     a, b = (Shared([100, 0, 33, 0, 16, 0], pages, blocks, page, np.random.default_rng(1)) for _ in range(2))
     lens, parents, new = i32(a.lens), i32(list(range(R))), i32(a.lens)
     out = (lens, torch.empty(R, 2, dtype=torch.int32, device="cuda"), torch.empty(4, dtype=torch.int32, device="cuda"))
@@ -546,14 +551,14 @@ def test_forks_as_lens_itself_and_captured(ea):  # noqa: F811
 
 
 @pytest.mark.parametrize("R,blocks,page,pages,shares", [(1, 1, 16, 1, True), (1, 2, 16, 2, False), (3, 5, 64, 31, True), (20, 9, 32, 64, True),
-                                                        (100, 7, 16, 1025, False), (300, 40, 16, 70000, True)])
+                                                        (100, 7, 16, 1025, False), (300, 40, 16, 70000, True), (2, 3, 16, 600000, True)])
 def test_compaction_against_the_reference(ea, R, blocks, page, pages, shares):  # noqa: F811
     rng = np.random.default_rng(R + pages)
     most = min(blocks, pages // R)
     s = Shared([int(n) for n in rng.integers(0, most * page + 1, R)], pages, blocks, page, rng)
     if shares:
         s.fork(ea, *ref.random_fork(rng, s.lens))
-    raw = garbage(pages, 1, 64, 16, pages)
+    raw = np.random.default_rng(pages).integers(0, 256, (pages, 1, 64), dtype=np.uint8)      # (pages of 64 bytes: what stands in them is all the same)
     cache = torch.from_numpy(raw).cuda()
     held = [[raw[p] for p in s.want.table[r][:s.want.size(n)]] for r, n in enumerate(s.lens)]
     before = [t.clone() for t in (s.table, s.free, s.shares)]
