@@ -401,7 +401,14 @@ template <class C, int D> void paged_entmax(const PagedParams& p, hipStream_t s)
     const long heads = (long)p.R * p.Hq;
     if (heads <= 64) paged_entmax_launch<C, D, 8, 4>(p, s);
     else if (heads < 512) paged_entmax_launch<C, D, 8, 1>(p, s);
-    else paged_entmax_launch<C, D, 4, 1>(p, s);
+    else {
+        // Two waves for many heads with few keys each.  Packed scores (the 8-bit cache), us with four / two waves at 1000, 4000 and 8000 keys:
+        //   640 heads 8.6 / 8.2, 10.0 / 11.0, 11.6 / 14.1;  1024: 9.2 / 8.5, 11.2 / 12.2, 12.7 / 14.0;  2048: 14.6 / 10.4, 17.3 / 14.0, 19.7 / 18.2
+        if constexpr (C::PACKED) {
+            if (2l * p.span <= 5 * heads) return paged_entmax_launch<C, D, 2, 1>(p, s);
+        }
+        paged_entmax_launch<C, D, 4, 1>(p, s);
+    }
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
