@@ -490,20 +490,22 @@ def _cache_args(call, cache, d, page_size):
     return cache.shape[0], cache.shape[1]
 
 
-def _token_strides(t):
-    a, b, _ = t.stride()
+def _token_strides(shape, strides):
+    a, b, _ = strides
     if (a | b) & 7:         # (as in _row_strides)
-        a, b = (0 if n == 1 else s for n, s in zip(t.shape, (a, b)))
+        a, b = (0 if n == 1 else s for n, s in zip(shape, (a, b)))
     return _TwoStrides(a, b)
 
 
 def _cache_rows(call, k, v, slots, Hk):
-    if k.dim() != 3 or k.shape != v.shape or k.shape[1] != Hk or k.dtype != v.dtype:
+    shape = k.shape
+    if len(shape) != 3 or shape != v.shape or shape[1] != Hk or k.dtype != v.dtype:
         raise ValueError(f"{call}: K, V must be [T,Hk,d] of one dtype, with the cache's Hk")
-    if k.numel() and (k.stride(2) != 1 or v.stride(2) != 1):
+    ks, vs = k.stride(), v.stride()
+    if (ks[2] != 1 or vs[2] != 1) and k.numel():
         raise ValueError(f"{call}: the elements of a row must be contiguous")
-    _int32(call, "slots", slots, (k.shape[0],))
-    return _token_strides(k), _token_strides(v)
+    _int32(call, "slots", slots, shape[:1])
+    return _token_strides(shape, ks), _token_strides(shape, vs)
 
 
 def entmax_attn_cache4_write(K, V, slots, cache, page_size):
@@ -581,9 +583,10 @@ def entmax_attn_cache8_empty(n_pages, Hk, d, page_size, device="cuda"):
 
 
 def _cache8_args(call, cache, d, page_size):
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.shape[2] != 2 * page_size * d + max(16, page_size // 2):
+    shape = cache.shape
+    if cache.dtype != torch.uint8 or len(shape) != 3 or not cache.is_contiguous() or shape[2] != 2 * page_size * d + max(16, page_size // 2):
         raise ValueError(f"{call}: cache must be contiguous uint8 [n_pages, Hk, 2 page_size d + max(16, page_size / 2)]")
-    return cache.shape[0], cache.shape[1]
+    return shape[0], shape[1]
 
 
 def entmax_attn_cache8_write(K, V, slots, cache, page_size):
