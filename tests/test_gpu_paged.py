@@ -235,6 +235,10 @@ DECODE = [
     ([7 * i for i in range(40)], 16, 2, 64, "bf16", 64, 1.5, 1.5),             # 640 heads: four waves each in the second kernel
     ([33 * i for i in range(1, 34)], 16, 1, 128, "bf16", 32, 1.25, 1.0),
     ([50000], 8, 2, 64, "bf16", 128, 1.5, 1.5),
+    ([70000], 8, 2, 128, "f32", 64, 1.5, 1.5),                 # sixteen waves in the second kernel
+    ([70000], 2, 1, 64, "bf16", 256, 1.5, 0.2),                # and flat
+    ([3 * i for i in range(70)], 32, 4, 64, "bf16", 16, 1.5, 1.5),             # 2240 heads: two waves each
+    ([9 * i for i in range(70)], 16, 1, 128, "f32", 32, 2.0, 0.3),             # 1120, flat
 ]
 
 
