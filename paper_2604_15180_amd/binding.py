@@ -707,8 +707,10 @@ def entmax_attn_cache_compact(lens, block_table, free_pages, free_count, shares,
     dev = _on_gpu(call, lens, block_table, free_pages, free_count, shares, workspace, *(out or ()))
     R, blocks, pages = _tables_args(call, lens, block_table, free_pages, free_count, shares)
     if out is None:
-        out = (torch.empty_like(block_table), torch.empty_like(free_pages), None if shares is None else torch.empty_like(shares),
-               lens.new_empty((pages // 2, 2)), lens.new_empty(4))
+        some = 0 if shares is None else pages
+        moves, tables, stack, held, status = torch.empty(2 * (pages // 2) + R * blocks + pages + some + 4, dtype=torch.int32,
+                                                         device=lens.device).split_with_sizes([2 * (pages // 2), R * blocks, pages, some, 4])
+        out = tables.view(R, blocks), stack, held if some else None, moves.view(pages // 2, 2), status
     else:
         if (out[2] is None) != (shares is None):
             raise ValueError(f"{call}: shares and its output go together")

@@ -263,6 +263,8 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
 // takes as a whole for one head's keys or values.  The rows in front of a run's first keep their codes, unless the run's own scale is
 // larger than the block's: then it becomes the block's, and they are rounded once more.  A run that begins with row 0
 // begins its block.
+// Bound: HBM for a prompt: 16001 tokens of 16 rows of 128 values are written in 22.2 us, 4.4 TB/s of reads and writes together, and read back in 18.5,
+// 5.3 TB/s; 64 tokens 4.5 and 3.2 us, chains slots -> rows, scale and kept codes -> codes.
 // The nearest integer n is that of x times 1 / s, which is off by up to 2^-16; the remainder x - n s, exact in one fused
 // multiply-add, then tells whether n is the one (halves are exact, too).  It hardly ever is not, nor is a value: both are looked at
 // for all of a lane's values at once, and put right in a branch of their own.  Kept codes: c s_old = p + e with two floats, and

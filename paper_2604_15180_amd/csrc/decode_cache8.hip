@@ -84,8 +84,13 @@ EA_DEV void query_digits(const QRow<E, D>& row, int wave, int (*words)[8][64], f
 }
 
 // Tiles of sixteen keys, one instruction per term and 64 elements.  Result: lane (n, g) holds column n's scores with keys
-// 4 g .. 4 g + 3.  A wave keeps two blocks of 64 keys on their way: as soon as the matrix cores have taken a tile, the same tile of the
-// block after the next is requested.  The addresses and scales of all its tiles are formed and loaded at once, a lane for each.
+// 4 g .. 4 g + 3.  A wave keeps a block of 64 keys on its way: as soon as the matrix cores have taken a tile, the same tile of the
+// next block is requested.  The addresses and scales of all its tiles are formed and loaded at once, a lane for each.
+// At D = 128 an operand is half a row, but a load is of eight whole rows (half lines cost 15 %): lane (n, g) loads of row n mod 8, then of row
+// n mod 8 + 8, piece g, or piece 4 + g in the lanes n >= 8, and the two halves of sixteen lanes exchange what is the other's.
+// Bound: HBM, for long requests: one of 131072 keys with 32 key heads takes 93 us, 5.8 TB/s of keys; 48 requests up to 32768 keys 63 us, 4.3 TB/s;
+// 64 with a window of 4000, 34 us, 4.0 TB/s.  One block ahead leaves registers for three or four waves per SIMD (two blocks: two waves, 104
+// us and 74 for 102 and 72 before the scores were packed).
 template <class E, int D>
 __global__ __launch_bounds__(64 * PD_WAVES, 3) void cache8_scores_kernel(PagedParams p) {
     constexpr int NT = sizeof(typename E::elem) == 2 ? 3 : 4, RUNS = D / 64, U = PD_BLOCK / 16;
@@ -138,7 +143,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, 3) void cache8_scores_kernel(PagedPa
 #pragma unroll
         for (int run = 0; run < RUNS; ++run) x.a[u][run] = __builtin_nontemporal_load((global_codes)(rows + lrow + 1024 * run));
     };
-    auto operands = [&](i32x4 (&a)[RUNS]) {
+    auto operands = [&](i32x4 (&a)[RUNS]) {               // (row_ror 8: from the lane n + 8 or n - 8 of the same sixteen)
         if constexpr (RUNS == 2) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
