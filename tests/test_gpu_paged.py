@@ -176,6 +176,35 @@ def test_rows_skipped_and_out_of_order(ea):  # noqa: F811
     assert torch.equal(cache, untouched)
 
 
+@pytest.mark.parametrize("T", [80, 5000])
+def test_rows_of_one_slot_or_apart_leave_other_blocks_alone(ea, T):  # noqa: F811
+    # what the header leaves undefined stays inside the blocks concerned: one slot forty times, rows of a block apart from each other
+    Hk, d, page = 4, 64, 32
+    rng = np.random.default_rng(T)
+    pages = T // page + 4
+    cache, want = pair(pages, Hk, d, page, seed=T)
+    slots = list(range(2 * page, 2 * page + T))
+    for i in range(40):
+        slots[20 + i] = 5                                         # block 0
+    slots[70], slots[75] = 17, 20                                 # block 1, apart, in the middle of other rows
+    fine = [s if s >= 2 * page else -1 for s in slots]
+    k, v = rows_of(rng, T, Hk, d, "bf16"), rows_of(rng, T, Hk, d, "bf16")
+    ea.entmax_attn_cache8_write(k.cuda(), v.cuda(), i32(slots), cache, page)
+    want.write(k.float().numpy(), v.float().numpy(), fine)
+    got, ref_bytes = cache.cpu().numpy(), want.bytes()
+    hurt = {s // 16 for i, s in enumerate(slots) if s < 2 * page or any(0 <= j < T and slots[j] < 2 * page for j in (i - 1, i + 1))}
+    hurt |= {(2 * page + i) // 16 for i in (20, 60, 70, 75)}
+    n = page * d
+    for b in range(pages * page // 16):
+        if b in hurt:
+            continue
+        pg, at = b * 16 // page, b * 16 % page
+        for o in (0, n):
+            np.testing.assert_array_equal(got[pg, :, o + at * d:o + (at + 16) * d], ref_bytes[pg, :, o + at * d:o + (at + 16) * d])
+        for o in (2 * n + 4 * (at // 16), 2 * n + 4 * (page // 16 + at // 16)):
+            np.testing.assert_array_equal(got[pg, :, o:o + 4], ref_bytes[pg, :, o:o + 4])
+
+
 def test_rows_of_any_stride(ea):  # noqa: F811
     Hk, d, page = 3, 64, 16
     rng = np.random.default_rng(4)
@@ -618,6 +647,31 @@ def test_copies_of_pages(ea):  # noqa: F811
             assert torch.equal(cache, want)
     with pytest.raises(ValueError):
         ea.entmax_attn_cache_copy(cache, moves, i32([1]), dst=cache[:, :4].contiguous())
+
+
+def test_pages_on_another_stream(ea):  # noqa: F811
+    # fork, copies and compaction enqueued on a stream of their own behind a long kernel, with the default stream idle
+    rng = np.random.default_rng(11)
+    s = Shared([100, 0, 33, 0], 60, 3000, 16, rng)
+    cache = torch.from_numpy(garbage(60, 1, 64, 16, 3)).cuda()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        a = torch.randn(2048, 2048, device="cuda")
+        for _ in range(20):
+            a = (a @ a).clamp(-1, 1)
+        parents, new, lens = i32([0, 0, 2, 2]), i32([100, 90, 33, 33]), i32(s.lens)
+        out = ea.entmax_attn_cache_fork(lens, parents, new, s.table, s.free, s.count, s.shares, 16)
+        ea.entmax_attn_cache_copy(cache, out[1], out[2][:1])
+        packed = ea.entmax_attn_cache_compact(out[0], s.table, s.free, s.count, s.shares, 16)
+        ea.entmax_attn_cache_copy(cache, packed[3], packed[4][:1])
+    side.synchronize()
+    want, moves, status = s.want.fork(s.lens, [0, 0, 2, 2], [100, 90, 33, 33])
+    assert out[0].tolist() == want and out[2].tolist() == status and out[1].tolist()[:len(moves)] == [list(m) for m in moves]
+    s.check()
+    moved, used = s.want.compact(want)
+    assert packed[4].tolist() == [len(moved), used, 0, 0] and packed[3].tolist()[:len(moved)] == [list(m) for m in moved]
+    np.testing.assert_array_equal(packed[0].cpu().numpy(), np.array(s.want.table))
 
 
 # ---- in turn ------------------------------------------------------------------------------------------------------
