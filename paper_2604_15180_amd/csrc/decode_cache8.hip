@@ -193,9 +193,11 @@ __global__ __launch_bounds__(64 * PD_WAVES, 3) void cache8_scores_kernel(PagedPa
         float quad[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (!whole) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (!whole && !seen(t0 + 16 * u + 4 * g + k)) s[u][k] = -INFINITY;
+                for (int k = 0; k < 4; ++k)
+                    if (!seen(t0 + 16 * u + 4 * g + k)) s[u][k] = -INFINITY;
+            }
             quad[u] = fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3]));
             best = fmaxf(best, quad[u]);
         }
