@@ -316,6 +316,7 @@ def entmax_attn_decode(q, K, V, alpha, workspace=None):
 # making a Stream object (entmax_attn_cache_tables: 14.6 -> 11.4 us of host time a call,
 # of which the launch is 3).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _on_gpu(call, first, *others):
@@ -333,7 +334,7 @@ def _on_gpu(call, first, *others):
 
 def _launch(dev, function, *args):
     """Calls the library with `args` and the current stream of device `dev`, with that device current."""
-    before = torch.cuda.current_device()
+    before = _current_device()
     if before == dev:
         rc = function(*args, _raw_stream(dev))
     else:
@@ -608,8 +609,10 @@ def entmax_attn_cache8_read(cache, slots, page_size, d, dtype=torch.bfloat16, ou
     dev = _on_gpu(call, cache, slots, *(out or ()))
     pages, Hk = _cache8_args(call, cache, d, page_size)
     if out is None:
-        out = (cache.new_empty((slots.numel(), Hk, d), dtype=dtype), cache.new_empty((slots.numel(), Hk, d), dtype=dtype))
-    K, V = out
+        K = torch.empty(slots.numel(), Hk, d, dtype=dtype, device=cache.device)      # (sizes as a tuple: 0.4 us more)
+        V = torch.empty_like(K)
+    else:
+        K, V = out
     if K.shape[-1] != d:
         raise ValueError(f"{call}: out must be [T,Hk,{d}]")
     ks, vs = _cache_rows(call, K, V, slots, Hk)
@@ -634,12 +637,14 @@ def entmax_attn_decode_cache8(q, cache, block_table, lens, alpha, page_size, max
     R, Hq, d = q.shape
     window, sinks = min(window, _INT_MAX), min(sinks, _INT_MAX)         # (no request is longer)
     pages, Hk = _cache8_args(call, cache, d, page_size)
-    _int32(call, "block_table", block_table, (R, block_table.shape[1]))
-    _int32(call, "lens", lens, (R,))
     blocks = block_table.shape[1]
+    _int32(call, "block_table", block_table, (R, blocks))
+    _int32(call, "lens", lens, (R,))
     if max_len is None:
         max_len = blocks * page_size
-    O, tau, support = q.new_empty((R, Hq, d), dtype=torch.float32), q.new_empty((R, Hq), dtype=torch.float32), lens.new_empty((R, Hq))
+    O = torch.empty(R, Hq, d, dtype=torch.float32, device=q.device)
+    tau = torch.empty(R, Hq, dtype=torch.float32, device=q.device)
+    support = torch.empty_like(tau, dtype=torch.int32)
     ws = workspace
     if ws is None:
         ws = _workspace(entmax_attn_decode_cache8_workspace_bytes(R, Hq, Hk, d, max_len, window, sinks), q.device)
