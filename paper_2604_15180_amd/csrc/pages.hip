@@ -23,7 +23,7 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 // does all of it, for its steps to be a barrier apart and not a launch.  More are FORK_GROUPS work-groups' work where it counts, since a
 // compute unit handles about one address a clock where they are all different: there are four launches then, by FORK_STEP.
 // 64 requests, 56 of them new with 1700 pages of 8 prompts: 12 us in one launch, 16 in four (with the ending and the copies 31.1 us a pass and 51.0);
-// 1020 with 45000 pages of 60 prompts: 130 us in one, 22 in four, and their end 162 and 40.
+// 1020 with 45000 pages of 60 prompts: 130 us in one, 22 in four, and their end 162 and 34.
 
 constexpr int FORK_THREADS = 1024;
 constexpr int FORK_MAX_REQUESTS = 4096;
@@ -76,7 +76,9 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
     __shared__ int32_t prefix[2][MAX + 1];                      // entries taken over and left by the requests in front
     __shared__ uint16_t from[MAX];
     __shared__ unsigned int ends[MAX], best[MAX];
-    __shared__ int sums[2][NW], claims[2][64];
+    // claims a thread looks at at a time, their counts per lane (45000 claims, the last launch: 22.6 us with 4, 20.0 with 8, 18.6 with 16, 21.7 with 32)
+    constexpr int S = ALL ? 64 / NW : 256 / NW, PER = NW * S / 64;
+    __shared__ int sums[2][NW], claims[2][NW * S];
     __shared__ int invalid, strange;
     int32_t* const take = prefix[0];
     int32_t* const leave = prefix[1];
@@ -197,7 +199,6 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
     if constexpr (ALL || STEP == FORK_FINISH) {
         const int count = min(max(*p.free_count, 0), p.n_pages);
         // the stack: claims from the last entry to the first, S of a thread's at a time and the next on their way
-        constexpr int S = 64 / NW;
         const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         int back = 0, page[S], ahead[S];
         auto left_from = [&](int i0, int (&x)[S]) {
@@ -218,10 +219,13 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
                 if (lane == 0) claims[turn][u * NW + wave] = __popcll(in[u]);
             }
             __syncthreads();
-            const int n = claims[turn][lane], up_to = wave_scan(n);
+            int n = 0, at_wave = 0;                       // of the lane's counts; of those in front of its one of this wave
+#pragma unroll
+            for (int k = 0; k < PER; ++k) { const int c = claims[turn][PER * lane + k]; n += c; if (k < wave % PER) at_wave += c; }
+            const int up_to = wave_scan(n);
 #pragma unroll
             for (int u = 0; u < S; ++u) {
-                const int at = count + back + __builtin_amdgcn_readlane(up_to - n, u * NW + wave) + __popcll(in[u] & ((1ull << lane) - 1ull));
+                const int at = count + back + __builtin_amdgcn_readlane(up_to - n + at_wave, (u * NW + wave) / PER) + __popcll(in[u] & ((1ull << lane) - 1ull));
                 if (in[u] >> lane & 1) {
                     if (at < p.n_pages) p.free_pages[at] = page[u];
                     C::set(&p.shares[page[u]], 0);

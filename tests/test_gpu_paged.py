@@ -520,6 +520,18 @@ def test_forks_against_the_reference(ea, R, blocks, page, pages):  # noqa: F811
     assert s.count.item() == pages and s.shares.sum().item() == 0 and sorted(s.free.tolist()) == list(range(pages))
 
 
+def test_forks_that_leave_many_pages(ea):  # noqa: F811
+    # tens of thousands of entries left, with and without other holders: the stack is built in several pieces
+    rng = np.random.default_rng(16)
+    R, blocks, page = 300, 200, 16
+    s = Shared([int(n) for n in rng.integers(80 * page, blocks * page + 1, R)], 45000, blocks, page, rng)
+    s.fork(ea, [r if r < 150 else r - 150 for r in range(R)], [s.lens[r % 150] for r in range(R)])           # half of them leave theirs
+    s.fork(ea, *ref.random_fork(rng, s.lens))
+    s.fork(ea, list(range(R)), [n // 9 for n in s.lens])
+    s.fork(ea, list(range(R)), [0] * R)
+    assert s.count.item() == 45000 and s.shares.sum().item() == 0 and sorted(s.free.tolist()) == list(range(45000))
+
+
 @pytest.mark.parametrize("blocks", [4, 3000])                                # (one launch, four launches)
 def test_forks_where_no_page_is_left(ea, blocks):  # noqa: F811
     rng = np.random.default_rng(7)
