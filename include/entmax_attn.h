@@ -413,11 +413,12 @@ int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* b
  * entmax_attn_cache_compact: the pages in use move to the front: with `used` pages not on the stack, the i-th free page below `used` takes the
  * i-th page in use from `used` on.  Every output may be its input itself.
  *   table_out   out    [R][max_blocks]: block_table with the pages' new ids, all other entries as they were
- *   free_out    out    [n_pages]: the stack of the free pages, the lowest on top; entries behind it as they were
+ *   free_out    out    [n_pages]: the stack of the free pages, the lowest on top, and -1 at its bottom for each of its entries that was out of range or
+ *               on it already (free_count stays, and no page in use is on the stack); entries behind it as they were
  *   shares_out  out    [n_pages] (0 for a free page); NULL if shares is
  *   moves       out    [n_pages / 2][2] int32, 8-byte aligned: from and to, -1 behind the last; no page that is moved from is moved to
  *   status      out    [4] int32: moves, pages in use, lengths out of range (their tables stay), page ids that are out of range, twice on the
- *               stack, or free but in a table (such entries stay)
+ *               stack, or free but in a table (a table's entries of this kind stay)
  *
  * entmax_attn_cache_copy: pages moves[i] = (from, to), i < count[0] and i < max_moves, of page_bytes (a multiple of 16) bytes each, from `src` to `dst`, which may
  * be one cache if no page is both, nor the target of two.  Pairs with an id out of range are skipped.

@@ -392,9 +392,11 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_move_kernel(CompactPa
         return page < used ? page : p.holes[(page - used) - (free_before(p, page) - free_before(p, used))];
     };
     if (id < p.n_pages) {
-        const int page = (int)id, holes = used < p.n_pages ? free_before(p, used) : 0, free = p.before[p.words];
+        const int page = (int)id, holes = used < p.n_pages ? free_before(p, used) : 0;
+        // entries of the stack, and how many of them are no page or one that is on it already: -1 in their place, taken last of all
+        const int stack = compact_free(p), empty = stack - p.before[p.words];
         if (page < p.n_pages / 2 && page >= holes) *(i32x2*)(p.moves + 2 * page) = i32x2{-1, -1};
-        p.free_out[page] = page < free ? p.n_pages - 1 - page : p.free_pages[page];
+        p.free_out[page] = page < empty ? -1 : page < stack ? p.n_pages - 1 - (page - empty) : p.free_pages[page];
         if (p.shares) {
             // (a page's count is read and written by one thread, and a moved one's by the page that it moves from)
             if (page >= used) {

@@ -1,0 +1,65 @@
+"""Accounts of shared pages where something is wrong."""
+import pytest
+import torch
+
+from tests.test_gpu_operators import ea, i32  # noqa: F401  (ea: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- compaction ---------------------------------------------------------------------------------------------------
+
+def stack_after(free, count, pages):
+    """What a compaction makes of a stack: its distinct pages in range, the lowest on top, and below them -1 for each other entry."""
+    live = min(max(count, 0), pages)
+    good = len({p for p in free[:live] if 0 <= p < pages})
+    return [-1] * (live - good) + [pages - 1 - i for i in range(good)] + free[live:]
+
+
+def test_no_page_in_use_is_on_the_stack_after_a_compaction(ea):  # noqa: F811
+    # an id out of range on the stack; the pages that are free are granted first, then the entry is met and counted
+    page, pages = 16, 8
+    free = i32([99, 6, 7, 1, 0, 0, 0, 0])
+    table = i32([[0, 2, 3, 4, 5], [-1] * 5])
+    lens, count = i32([80, 0]), i32([4])
+    out = ea.entmax_attn_cache_compact(lens, table, free, count, None, page)
+    assert out[0].tolist() == [[0, 2, 3, 4, 1], [-1] * 5] and out[4].tolist() == [1, 5, 0, 1]
+    assert out[1].tolist() == [-1, 7, 6, 5, 0, 0, 0, 0]
+    step = ea.entmax_attn_cache_tables(lens, i32([80, 48]), out[0], out[1], count, page, 48)
+    assert out[0].tolist() == [[0, 2, 3, 4, 1], [5, 6, 7, -1, -1]]
+    assert step[-1].tolist()[3] == 0 and count.item() == 1
+    step = ea.entmax_attn_cache_tables(i32([80, 48]), i32([80, 64]), out[0], out[1], count, page, 16)
+    assert out[0].tolist()[1] == [5, 6, 7, -1, -1] and step[2].tolist() == [-1] * 16 and step[-1].tolist()[3] == 1
+
+
+@pytest.mark.parametrize("free,count,lens,table", [
+    ([4, 4, 11, -1, 5, 6, 2, 0, 0, 0], 7, [48, -1, 100], [[0, 5, 9], [3, 8, 1], [7, 7, 7]]),
+    ([5, 6, 7, 8, 9, 5, 6, 7, 8, 9], 25, [48, 32, 0], [[0, 1, 2], [3, 4, 0], [0, 0, 0]]),       # (a count above the number of pages)
+    ([5, 5, 5, 5, 5, 5, 5, 5, 5, 5], 10, [48, 0, 0], [[7, 8, 9], [0, 0, 0], [0, 0, 0]]),
+    ([10, -1, 10, -1, 3, 2, 1, 0, 0, 0], 4, [48, 0, 0], [[7, 8, 9], [0, 0, 0], [0, 0, 0]]),
+    ([6, 7, 3, 2, 1, 0, 9, 8, 5, 4], -3, [48, 0, 0], [[7, 8, 9], [0, 0, 0], [0, 0, 0]]),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_stacks_that_do_not_add_up(ea, free, count, lens, table, in_place):  # noqa: F811
+    pages = len(free)
+    t, f, c = i32(table), i32(free), i32([count])
+    moves, status = torch.empty(pages // 2, 2, dtype=torch.int32, device="cuda"), torch.empty(4, dtype=torch.int32, device="cuda")
+    out = ea.entmax_attn_cache_compact(i32(lens), t, f, c, None, 16, out=(t, f, None, moves, status) if in_place else None)
+    live = min(max(count, 0), pages)
+    want = stack_after(free, count, pages)
+    assert out[1].tolist() == want and c.item() == count
+    used = pages - len({p for p in free[:live] if 0 <= p < pages})
+    assert out[4].tolist()[1] == used
+    # every entry that can be popped is a page behind those in use, each once, or none at all
+    popped = [p for p in out[1].tolist()[:live] if p != -1]
+    assert sorted(popped) == list(range(used, pages))
+
+
+def test_a_large_stack_that_does_not_add_up(ea):  # noqa: F811
+    # (its bits are not made in LDS)
+    pages = 600000
+    free = list(range(pages - 1, 49, -1)) + [100, 70, 50, -9, pages] + [0] * 45
+    table = i32([[49, 48, 47, 0], [1, 2, 3, 4]])
+    out = ea.entmax_attn_cache_compact(i32([64, 64]), table, i32(free), i32([pages - 45]), None, 16)
+    assert out[1].tolist() == stack_after(free, pages - 45, pages)
+    assert out[4].tolist() == [0, 50, 0, 5] and torch.equal(out[0], table)
