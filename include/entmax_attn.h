@@ -300,7 +300,8 @@ int entmax_attn_qk_norm_rope_bwd(const void* q, const void* k, const float* dq_o
  *   slots, positions out [max_tokens] int32: each row's slot and position in its request; slot -1 in the rows of a
  *                      request that was refused, and slot -1, position 0 in the rows behind the last
  *   status      out    [4] int32: rows in use (at most max_tokens), requests refused, requests with a length that is negative or
- *                      above max_blocks * page_size (nothing is done for them), page ids outside 0 .. n_pages - 1 met
+ *                      above max_blocks * page_size (nothing is done for them), page ids outside 0 .. n_pages - 1 met, and pages
+ *                      given back to a stack that held n_pages already (free_count was wrong; such pages are lost)
  * A request that wants more pages than are left after the requests before it, or whose rows end behind max_tokens, is
  * refused whole: its length and pages stay, and so it is for the later ones that want any (pages; rows).  R <= 4096,
  * max_blocks * page_size <= 2^22.  The pages of a request must be its own: the call cannot tell.
@@ -407,7 +408,7 @@ int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* b
  *               ends before the page that was to be copied
  *   moves       out    [R][2] int32, 8-byte aligned: pages to be copied, from and to, before either is written to; -1 behind the last
  *   status      out    [4] int32: moves, requests for whose copy no page was left, requests that stay as they are because of
- *               their arguments, page ids outside 0 .. n_pages - 1 met
+ *               their arguments, page ids outside 0 .. n_pages - 1 met, and pages that the stack had no room for (as there)
  *   workspace   entmax_attn_cache_fork_workspace_bytes bytes, 256-byte aligned
  *
  * entmax_attn_cache_compact: the pages in use move to the front: with `used` pages not on the stack, the i-th free page below `used` takes the

@@ -228,6 +228,7 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
                 const int at = count + back + __builtin_amdgcn_readlane(up_to - n + at_wave, (u * NW + wave) / PER) + __popcll(in[u] & ((1ull << lane) - 1ull));
                 if (in[u] >> lane & 1) {
                     if (at < p.n_pages) p.free_pages[at] = page[u];
+                    else atomicAdd(&strange, 1);          // (the stack was full: its count was none of free pages)
                     C::set(&p.shares[page[u]], 0);
                 }
             }

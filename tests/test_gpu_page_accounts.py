@@ -63,3 +63,26 @@ def test_a_large_stack_that_does_not_add_up(ea):  # noqa: F811
     out = ea.entmax_attn_cache_compact(i32([64, 64]), table, i32(free), i32([pages - 45]), None, 16)
     assert out[1].tolist() == stack_after(free, pages - 45, pages)
     assert out[4].tolist() == [0, 50, 0, 5] and torch.equal(out[0], table)
+
+
+# ---- forks --------------------------------------------------------------------------------------------------------
+
+PATHS = pytest.mark.parametrize("blocks", [5, 9000])            # (one launch, four launches)
+
+
+def padded(rows, blocks):
+    return i32([r + [-1] * (blocks - len(r)) for r in rows])
+
+
+@PATHS
+def test_pages_that_the_stack_has_no_room_for_are_counted(ea, blocks):  # noqa: F811
+    # a count that says 7 of 8 pages are free while a request holds three: two of them find no place
+    table, free, count, shares = padded([[0, 1, 2], [], []], blocks), i32([3, 4, 5, 6, 7, 3, 4, -5]), i32([7]), i32([0] * 8)
+    out = ea.entmax_attn_cache_fork(i32([48, 0, 0]), i32([0, 1, 2]), i32([0, 0, 0]), table, free, count, shares, 16)
+    assert out[2].tolist() == [0, 0, 0, 2] and out[0].tolist() == [0, 0, 0]
+    assert count.item() == 8 and free.tolist() == [3, 4, 5, 6, 7, 3, 4, 2] and shares.tolist() == [0] * 8
+    # beside ids out of range, which are met as well
+    table, free, count, shares = padded([[0, 9, 2], [1], []], blocks), i32([3, 4, 5, 6, 7, 3, 4, -5]), i32([100]), i32([0] * 8)
+    out = ea.entmax_attn_cache_fork(i32([48, 16, 0]), i32([0, 1, 2]), i32([0, 16, 0]), table, free, count, shares, 16)
+    assert out[2].tolist() == [0, 0, 0, 3] and out[0].tolist() == [0, 16, 0]
+    assert count.item() == 8 and free.tolist() == [3, 4, 5, 6, 7, 3, 4, -5]
