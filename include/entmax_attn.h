@@ -398,7 +398,7 @@ int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* b
  * entmax_attn_cache_fork: request r becomes the first new_lens[r] tokens of what request parents[r] held before the call, all
  * requests at once: itself shortened (parents[r] = r), ended (0), left as it is (its own length), or a fork of another.
  *   lens, parents, new_lens in [R] int32; a request with a parent that is none, a new length that is negative or above its parent's, or a length of its own
- *               that is negative or above max_blocks * page_size stays as it is
+ *               that is negative or above max_blocks * page_size stays as it is, to its last token and page (others that end in that page get copies)
  *   block_table, free_pages, free_count in/out as in entmax_attn_cache_tables.  First the pages that nobody holds any more go on top of the
  *               stack, the last request's last page first (a page that several requests leave counts as the last one's).  Then each
  *               request that ends inside a page that others hold too gets a page of its own from the top, in order; one of those that end in a page

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
     using C = Counts<STEP>;
     constexpr bool ALL = STEP == FORK_ALL;
     constexpr int T = FORK_THREADS, NW = T / 64, U = STEP == FORK_COUNT || STEP == FORK_CLAIM ? 1 : FORK_AT_ONCE, MAX = FORK_MAX_REQUESTS, SLOTS = 2 * MAX;
-    __shared__ int32_t have[MAX], next[MAX], tail[MAX];         // lengths before and after; the page in whose middle a request ends, or -1
+    __shared__ int32_t have[MAX], next[MAX], tail[MAX];         // lengths before and after; the page in whose middle a request comes to end, or -1
     __shared__ int32_t prefix[2][MAX + 1];                      // entries taken over and left by the requests in front
     __shared__ uint16_t from[MAX];
     __shared__ unsigned int ends[MAX], best[MAX];
@@ -101,17 +101,19 @@ __global__ __launch_bounds__(FORK_THREADS) void cache_fork_kernel(ForkParams p) 
             int parent = r < R ? p.parents[r] : 0, len = r < R ? p.new_lens[r] : 0;
             if (r0 == 0) __syncthreads();
             if (r < R) {
-                // a request whose lengths or parent are out of range stays as it is (and one whose own length is takes part in nothing)
+                // a request whose lengths or parent are out of range stays as it is, its last page among those that are held whole (and one whose
+                // own length is takes part in nothing)
                 const bool mine = have[r] >= 0 && have[r] <= most;
                 const int theirs = have[min(max(parent, 0), R - 1)];
-                if (!(mine && (unsigned)parent < (unsigned)R && theirs <= most && len >= 0 && len <= theirs)) {
+                const bool stays = !(mine && (unsigned)parent < (unsigned)R && theirs <= most && len >= 0 && len <= theirs);
+                if (stays) {
                     parent = r;
                     len = mine ? have[r] : 0;
                     atomicAdd(&invalid, 1);
                 }
                 from[r] = (uint16_t)parent;
                 next[r] = len;
-                tail[r] = tail_of(parent, len);
+                tail[r] = stays ? -1 : tail_of(parent, len);
                 const int old = mine ? pages_of(have[r], shift) : 0, now = pages_of(len, shift);
                 a = parent == r ? 0 : now;
                 b = !mine ? 0 : parent == r ? old - now : old;

@@ -86,3 +86,37 @@ def test_pages_that_the_stack_has_no_room_for_are_counted(ea, blocks):  # noqa: 
     out = ea.entmax_attn_cache_fork(i32([48, 16, 0]), i32([0, 1, 2]), i32([0, 16, 0]), table, free, count, shares, 16)
     assert out[2].tolist() == [0, 0, 0, 3] and out[0].tolist() == [0, 16, 0]
     assert count.item() == 8 and free.tolist() == [3, 4, 5, 6, 7, 3, 4, -5]
+
+
+@PATHS
+@pytest.mark.parametrize("left", [0, 2])
+def test_requests_with_arguments_out_of_range_stay_as_they_are(ea, blocks, left):  # noqa: F811
+    # two or three requests end in one page; those with bad arguments keep it, and who else ends in it gets the copy, or ends before it
+    rows = [[0, 1], [0, 1], [0, 1], [2]]
+    lens = [20, 20, 20, 5]
+    for parents, new, stay in (([0, 1, 2, 3], [20, 21, 0, 5], [1]), ([0, 4, 2, 3], [0, 20, 20, 5], [1]), ([0, -1, 2, 3], [20, 3, -1, 5], [1, 2]),
+                               ([0, 0, 0, 3], [21, 21, 21, 6], [0, 1, 2, 3]), ([1, 1, 2, 3], [19, 21, 0, 0], [1]), ([7, 0, 0, 0], [1, 18, 0, 17], [0])):
+        table, free, count = padded(rows, blocks), i32([6, 5, 4, 7, 3, -1, -1, -1]), i32([left])
+        shares = i32([2, 2, 0, 0, 0, 0, 0, 0])
+        out = ea.entmax_attn_cache_fork(i32(lens), i32(parents), i32(new), table, free, count, shares, 16)
+        got, tables, stat = out[0].tolist(), table.tolist(), out[2].tolist()
+        assert stat[2] == len(stay) and stat[3] == 0
+        moves = [m for m in out[1].tolist() if m != [-1, -1]]
+        assert stat[0] == len(moves)
+        for r in range(4):
+            if r in stay:
+                assert got[r] == lens[r] and tables[r] == (rows[r] + [-1] * blocks)[:blocks], (parents, r)
+            else:
+                assert got[r] == new[r] or (stat[1] and got[r] == new[r] // 16 * 16), (parents, r)
+        # accounts: every page's holders are counted, free pages are on the stack once, and who may write ends in a page of its own
+        held = [tables[r][:-(-got[r] // 16)] for r in range(4)]
+        live = free.tolist()[:count.item()]
+        for p in range(3):
+            k = sum(h.count(p) for h in held)
+            assert shares.tolist()[p] == max(k - 1, 0) and live.count(p) == (k == 0), (parents, p)
+        for r in range(4):
+            if r not in stay and got[r] % 16:
+                assert sum(h.count(held[r][-1]) for h in held) == 1, (parents, r)
+        # a copy comes from the page that its request would have ended in
+        for a, b in moves:
+            assert a in (0, 1, 2) and sum(h.count(b) for h in held) == 1
