@@ -628,7 +628,7 @@ def entmax_attn_decode_cache8_workspace_bytes(R, Hq, Hk, d, max_len, window=0, s
 def entmax_attn_decode_cache8(q, cache, block_table, lens, alpha, page_size, max_len=None, window=0, sinks=0, workspace=None):
     """entmax_attn_decode_cache4 against an 8-bit cache -> (O [R,Hq,d], tau [R,Hq], support [R,Hq]).  window > 0: a query sees
     the last `window` tokens of its request and the first `sinks`.  workspace: entmax_attn_decode_cache8_workspace_bytes bytes, about
-    4 R Hq min(max_len, window + sinks); without it they are allocated in every call."""
+    4.125 R Hq (n + 445) at most, n = max_len or with a window min(max_len, window + sinks); without it they are allocated in every call."""
     call = "entmax_attn_decode_cache8"
     _workspace_arg(call, workspace)
     dev = _on_gpu(call, q, cache, block_table, lens, workspace)
