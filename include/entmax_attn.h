@@ -367,6 +367,9 @@ int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* b
  * written, the block starts anew with s_new.  A code is x / s rounded to the nearest integer, an infinity or a NaN code -128.  What rows
  * behind the lowest one written held, and are not written themselves, is lost.  Where the slots of a call are not different, or rows of one block
  * stand apart, the codes and scales of that block are undefined.
+ * A value is off by at most half the scale that its row was written with and half of each larger scale that its block took on since: s / 2, 1/254 of
+ * the largest value (2^-119 or above), in a block that one call wrote; up to 8 s where sixteen calls wrote it and each brought a larger value than the
+ * ones before.  How the same tokens are cut into calls thus changes codes.
  *
  * entmax_attn_cache8_read: as entmax_attn_cache4_read; a value is code times scale in float32, rounded to `dtype`.
  *
