@@ -1,4 +1,5 @@
-"""Rows of the 8-bit cache on the GPU: what a block that grows in several calls has lost of the rows that were written."""
+"""Rows of the 8-bit cache on the GPU: what a block that grows in several calls has lost of the rows that were written, and every byte around
+slots that are skipped."""
 import numpy as np
 import pytest
 import torch
@@ -32,3 +33,19 @@ def test_rows_of_a_block_that_grows(ea, dtype, growth):  # noqa: F811
     got = ea.entmax_attn_cache8_read(cache, i32(list(range(16 * blocks))), page, d, torch.float32)
     worst = within_half_the_scales(scales, [t.cpu().numpy() for t in got], [x[:, :Hk].float().numpy(), x[:, Hk:].float().numpy()])
     print(f"  {growth} {dtype}: {calls} calls, largest error {worst:.1f} of 1/254 of a block's largest", flush=True)
+
+
+def test_all_bytes_around_skipped_slots(ea):  # noqa: F811
+    # slots that are negative or past the cache directly in front of and behind others, in blocks that hold finite rows already
+    Hk, d, page, pages = 2, 64, 32, 4
+    rng = np.random.default_rng(19)
+    want = ref.Cache8(np.zeros((pages, Hk, ref.part_bytes(d, page)), np.uint8), d, page)
+    cache = ea.entmax_attn_cache8_empty(pages, Hk, d, page)
+    for slots in (list(range(10)) + list(range(32, 43)) + list(range(64, 73)) + list(range(96, 100)) + list(range(112, 128)),
+                  [-1, 4 * page, 40, 41, -7, 70, 71, 2 ** 31 - 1, 127, 126, 125, 112, 0, -2 ** 31, 99, 98],
+                  [-1, 10, 11, 4 * page, -3, 43, -2 ** 31], [44, 2 ** 31 - 1, 72, 73, 74, -1, -1, 16]):
+        k, v = (torch.from_numpy((rng.standard_normal((len(slots), Hk, d)) * np.exp(rng.standard_normal((len(slots), 1, 1)))).astype(np.float32))
+                for _ in range(2))
+        ea.entmax_attn_cache8_write(k.cuda(), v.cuda(), i32(slots), cache, page)
+        want.write(k.numpy(), v.numpy(), slots)
+        np.testing.assert_array_equal(cache.cpu().numpy(), want.bytes())

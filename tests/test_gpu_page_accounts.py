@@ -1,7 +1,9 @@
-"""Accounts of shared pages where something is wrong."""
+"""Accounts of shared pages where something is wrong, and with holders that are none of a call's requests."""
+import numpy as np
 import pytest
 import torch
 
+from tests import paged_ref as ref
 from tests.test_gpu_operators import ea, i32  # noqa: F401  (ea: the fixture)
 
 pytestmark = pytest.mark.gpu
@@ -120,3 +122,56 @@ def test_requests_with_arguments_out_of_range_stay_as_they_are(ea, blocks, left)
         # a copy comes from the page that its request would have ended in
         for a, b in moves:
             assert a in (0, 1, 2) and sum(h.count(b) for h in held) == 1
+
+
+class State:
+    """The library's and the reference's tables, stack and holders, with holders that are none of the requests."""
+
+    def __init__(self, lens, pages, blocks, page, rng, pinned):
+        need = [-(-n // page) for n in lens]
+        order, at, table = rng.permutation(pages).tolist(), 0, []
+        for n in need:
+            table.append(order[at:at + n] + [-1] * (blocks - n))
+            at += n
+        shares = [0] * pages
+        for r, b in pinned:
+            shares[table[r][b]] += 1
+        self.want, self.lens, self.page = ref.Pages(table, order[at:], pages, page, shares), list(lens), page
+        self.table, self.free, self.count, self.shares = i32(table), i32(self.want.stack), i32([pages - at]), i32(shares)
+
+    def fork(self, ea, parents, new):  # noqa: F811
+        out = ea.entmax_attn_cache_fork(i32(self.lens), i32(parents), i32(new), self.table, self.free, self.count, self.shares, self.page)
+        lens, moves, status = self.want.fork(self.lens, parents, new)
+        assert out[0].tolist() == lens and out[2].tolist() == status
+        assert out[1].tolist() == [list(m) for m in moves] + [[-1, -1]] * (len(lens) - len(moves))
+        assert self.count.item() == self.want.count and self.free[:self.want.count].tolist() == self.want.stack[:self.want.count]
+        assert self.shares.tolist() == self.want.shares and torch.equal(self.table, i32(self.want.table))
+        self.lens = lens
+
+
+@pytest.mark.parametrize("blocks", [12, 9000])
+def test_forks_of_pages_that_others_hold_too(ea, blocks):  # noqa: F811
+    # a prefix that somebody outside the call holds, whole pages and the one in whose middle a request ends: it is copied, never
+    # written to, and its pages stay off the stack when all requests have ended
+    rng = np.random.default_rng(blocks)
+    lens = [100, 40, 33, 0, 7, 16]
+    pinned = [(0, b) for b in range(7)] + [(0, 6), (1, 0), (2, 2), (5, 0)]
+    s = State(lens, 90, blocks, 16, rng, pinned)
+    held = {s.want.table[r][b] for r, b in pinned}
+    s.fork(ea, list(range(6)), lens)                             # everybody who ends in such a page gets one of its own
+    assert all(s.want.table[r][s.lens[r] // 16] not in held for r in (0, 2))
+    for _ in range(6):
+        s.fork(ea, *ref.random_fork(rng, s.lens))
+    s.fork(ea, list(range(6)), [0] * 6)
+    assert not held & set(s.free[:s.count.item()].tolist())
+    assert s.count.item() == 90 - len(held) and s.shares.sum().item() == len(pinned) - len(held)
+
+
+def test_forks_of_more_entries_than_all_groups_take_at_a_time(ea):  # noqa: F811
+    rng = np.random.default_rng(12)
+    R, blocks, page, pages = 950, 300, 16, 5000
+    s = State([blocks * page] + [0] * (R - 1), pages, blocks, page, rng, [])
+    s.fork(ea, [0] * R, [blocks * page - (r % 3) * (r % 11) for r in range(R)])          # 284700 entries taken over
+    assert sum(-(-n // page) for n in s.lens[1:]) > 262144 + 16384
+    s.fork(ea, list(range(R)), [0] * R)                                                 # and left
+    assert s.count.item() == pages and s.shares.sum().item() == 0
