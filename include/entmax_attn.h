@@ -375,7 +375,8 @@ int entmax_attn_decode_cache4(const void* q, const void* cache, const int32_t* b
  *
  * entmax_attn_decode_cache8: as entmax_attn_decode_cache4, against this cache, and with a sliding window:
  *   window, sinks    with window > 0 the query of a request of length n sees the keys j with j >= n - window and those with j < sinks; with
- *                    window = 0 all.  Pages without a key that is seen are not read, nor are their entries of block_table.
+ *                    window = 0 all.  Pages without a key that is seen are not read, nor are their entries of block_table
+ *                    (they stay the request's: the calls that give pages back take them from its end).
  * The workspace is 4.125 R Hq n to 4.125 R Hq (n + 445) + 510 bytes, n = max_len or, with a window, the smaller of max_len and window + sinks: the keys are taken in
  * whole blocks of 64, and a head has room for three blocks more.  A head gets NaN and support -1 where its query, or a key that it sees, holds an
  * infinity or a NaN, where a page id that it needs is out of range, or where 2^floor(log2 max|q|) of its query times the scale of

@@ -273,7 +273,8 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(RowParams p, unsigned 
 // Tokens whose runs a wave looks after: 1 up to C8_FEW (tokens x heads of keys and values), 4 up to C8_MANY, 16 above.  One each keeps the
 // waves short, but of a prompt's only each sixteenth finds a run.  us with 1 / 4 / 16 tokens, 8 key heads of 128: 1400 requests with a token each
 // (22400) 16.7 / 16.2 / 25.3, 4000 (64000) 47.3 / 38.6 / 40.0; 8 chunks of 512 (50000) 22.0 / 13.4 / 10.4; chunks of 127, 5 heads of 64 (23000)
-// 7.4 / 6.0 / 6.0.
+// 7.4 / 6.0 / 6.0.  Around C8_FEW, 1 / 4: 8 key heads of 128, requests with a token each, 128 (2048) 4.3 / 7.2, 256 (4096) 5.0 / 7.8, 512 (8192) 7.6 / 8.8, 1024 (16384)
+// 11.8 / 11.7; one chunk of as many tokens 6.8 / 6.2, 7.9 / 6.4, 8.7 / 7.0 and 12.9 / 8.6: at 4096 tokens apart gain more than a chunk loses, at 8192 less.
 constexpr int C8_FEW = 1 << 12, C8_MANY = 1 << 15;
 
 // The float whose lowest byte is the nearest integer to x * inv, |x * inv| < 2^22; less C8_MAGIC it is that integer

@@ -400,7 +400,9 @@ template <class C, int D> void paged_entmax(const PagedParams& p, hipStream_t s)
     // The host knows neither the lengths nor the supports: the borders lie where short supports, the rule, begin to lose.
     const long heads = (long)p.R * p.Hq;
     // (The 8-bit cache's values are twice the bytes: sixteen waves for long requests of few heads.  One of 131072 keys, 32 heads: with short supports
-    // 12.8 us for 12.0 with eight, with flat scores 140 for 184, at alpha 1.05 459 for 728.)
+    // 12.8 us for 12.0 with eight, with flat scores 140 for 184, at alpha 1.05 459 for 728.  Around the border, both launches, 8 key heads, one request of normal
+    // queries and keys, alpha 1.5, a third of the queries, alpha 1.05, sixteen / eight: 65536 keys, 32 heads 43.9 / 52.0, 89 / 105, 206 / 305; 64 heads 47.7 / 57.1, 93 / 107, 223 / 308;
+    // 32768 keys, 32 heads 29.9 / 32.0, 65 / 65, 118 / 166: nearly alike but for long supports.)
     if constexpr (C::PACKED) {
         if (heads <= 64 && p.span >= 65536) return paged_entmax_launch<C, D, 16, 4>(p, s);
     }

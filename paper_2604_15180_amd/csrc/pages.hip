@@ -43,7 +43,11 @@ struct ForkParams {
 };
 
 enum FORK_STEP { FORK_ALL, FORK_LENGTHS, FORK_COUNT, FORK_CLAIM, FORK_FINISH };
-constexpr long FORK_ONE = 16384;        // (R * max_blocks: how many pages there are the host does not know)
+// (R * max_blocks: how many pages there are the host does not know.  A fork of 8 or 128 prompts to all requests and its end, replayed / from Python, us in one
+// launch and in four: 64 requests of 256 blocks with full tables 65 / 65 and 28 / 35, 1024 of 16 74 / 74 and 31 / 36; with tables 1/64 full 20 / 20 and 23 / 35,
+// 29 / 29 and 27 / 38.  At 65536 entries, full: 251 to 278 and 40 to 45; 1/64 full: 21 to 29 and 24 to 36.  The border is drawn for tables with room
+// to grow, where one launch saves the host three; full tables of 16384 entries are twice as fast in four.)
+constexpr long FORK_ONE = 16384;
 constexpr int FORK_GROUPS = 256, FORK_LIST = FORK_MAX_REQUESTS + 8;
 
 // (one work-group's scope will do for its own counts: across the card's L2s atomics take several times as long)
@@ -431,7 +435,8 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_move_kernel(CompactPa
 // ---- copies ---------------------------------------------------------------------------------------------------------
 // moves[i] = (from, to), the first `count` of them.  Bound: HBM, twice the pages' bytes.  A work-group copies 16 KB at a time, four
 // loads of 16 bytes a thread on their way together (eight: no faster).  Copies of more than COPY_FAR bytes in all bypass the caches: 2230 pages of
-// 132 KB, 589 MB read and written, take 118 us, 5.0 TB/s, for 127; 110 of them 7.9 us for 7.1.
+// 132 KB, 589 MB read and written, take 118 us, 5.0 TB/s, for 127; 110 of them 7.9 us for 7.1.  Around the border, pages of a cache of 3 GB: 61 MiB 27.1
+// past the caches and 27.1 through them, 121 MiB 52.9 and 54.9, 30 MiB 14.4 and 12.9.
 
 constexpr int COPY_U = 4, COPY_PIECE = 256 * COPY_U;      // of 16 bytes
 constexpr long COPY_FAR = 64l << 20;
