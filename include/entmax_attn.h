@@ -408,7 +408,7 @@ int entmax_attn_decode_cache8(const void* q, const void* cache, const int32_t* b
  *               stack, the last request's last page first (a page that several requests leave counts as the last one's).  Then each
  *               request that ends inside a page that others hold too gets a page of its own from the top, in order; one of those that end in a page
  *               keeps it, if none holds it whole: the first that is its own parent, else the first.  (New tokens may then be
- *               written to every request.)
+ *               written to every request but one that stays because of its arguments and ends in a page that others hold.)
  *   lens_out    out    [R] int32: the lengths now; may be `lens` itself, not parents or new_lens.  Where no page is left for a copy, the request
  *               ends before the page that was to be copied
  *   moves       out    [R][2] int32, 8-byte aligned: pages to be copied, from and to, before either is written to; -1 behind the last

@@ -703,7 +703,7 @@ def entmax_attn_cache_compact_workspace_bytes(n_pages):
 
 def entmax_attn_cache_compact(lens, block_table, free_pages, free_count, shares, page_size, out=None, workspace=None):
     """The pages in use move to the front of a cache -> (block_table, free_pages, shares, moves [n_pages / 2, 2], status [4]), int32:
-    the tables, the stack and the holders (None if shares is None) afterwards, and in moves[:status[0]] the pages to be copied with
+    the tables, the stack (free_count stays: -1 at its bottom for each entry that was no page or on it twice) and the holders (None if shares is None) afterwards, and in moves[:status[0]] the pages to be copied with
     entmax_attn_cache_copy(cache, moves, status[:1]).  `out`: tensors to write them into; the first three may be the inputs."""
     call = "entmax_attn_cache_compact"
     _workspace_arg(call, workspace)
